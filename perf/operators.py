@@ -213,7 +213,7 @@ def _run_own(st):
     fw.fw_gated_forward(st["X"], dt, N, M, S, st["Wg"], st["Wu"], st.get("bg"), st.get("bu"), st["act"], st["H"], st.get("Z"), st["ws"])
     if kind == "gated":
         return [st["H"]]
-    fw.fw_gated_grad(st["X"], dt, N, M, S, st["Wg"], st["Wu"], st["Z"], st["act"], st["dH"], st.get("mu"), st["dX"], st["dWg"],
+    fw.fw_gated_grad(st["X"], dt, N, M, S, st["Wg"], st["Wu"], st["Z"], st["dH"], st.get("mu"), st["dX"], st["dWg"],
                      st["dWu"], st.get("dbg"), st.get("dbu"), st["ws_grad"])
     return [st[k] for k in ("H", "dX", "dWg", "dWu") + (("dbg", "dbu") if case["bias"] else ())]
 
