@@ -6,7 +6,9 @@
  *   (1) accumulates the block sums behind the input moments  mu_x, Phi_x, phi_x   (Sec. 2, Sec. 4.1),
  *   (2) transforms the weight gradient  G -> G Q,  Q = T^T T                      (Sec. 3.1),
  *   (3) runs the recursive condition-number-reduction update of T, Q, Q_s         (Sec. 4),
- *   (4) builds the EVD / ZCA whitening matrix as the reference construction       (Sec. 2, Sec. 3.2).
+ *   (4) builds the EVD / ZCA whitening matrix as the reference construction       (Sec. 2, Sec. 3.2),
+ * and, for the layers of language models that are whitened,
+ *   (5) makes their input rows (norm), their products and weight gradients (gated block) and their answers in 8 bits.
  *
  * Conventions shared by every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller unless the comment says "host".
@@ -81,7 +83,8 @@ typedef struct { int B, Cin, H, W, kh, kw, stride, pad, form; } fw_conv_desc;
 /* Operations for fw_workspace_bytes. */
 typedef enum {
     FW_OP_COV_ACCUMULATE = 0, FW_OP_GRAD_TRANSFORM = 1, FW_OP_COND_REDUCE_STEP = 2, FW_OP_WHITEN_EVD = 3, FW_OP_COND_STATE_REFRESH = 4,
-    FW_OP_GRAD_TRANSFORM_TAPS = 5, FW_OP_SGD_UPDATE = 6, FW_OP_DIAGNOSTICS = 7, FW_OP_COND_PROBE = 8
+    FW_OP_GRAD_TRANSFORM_TAPS = 5, FW_OP_SGD_UPDATE = 6, FW_OP_DIAGNOSTICS = 7, FW_OP_COND_PROBE = 8,
+    FW_OP_RMS_NORM_GRAD = 9, FW_OP_GATED_FORWARD = 10, FW_OP_GATED_GRAD = 11, FW_OP_INT8_PRODUCT = 12
 } fw_op;
 
 /* ------------------------------------------------------------------------------------------------------------
@@ -352,6 +355,97 @@ fw_status fw_diagnostics(const float* Phi_y, const float* lambda, int M, float* 
 #define FW_COND_PROBE_MAX_K 32
 fw_status fw_cond_probe(const float* Phi_y, int M, const float* b0, int k, float* out, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * (5) Layers of a language model around the whitening: what makes a layer's input rows X [N, M] (one row per token, the rows that
+ * fw_cov_accumulate takes as FW_LAYOUT_ROWS), its products, its weight gradients G [S, M], and its answers in 8 bits.  N, M and S
+ * need not be multiples of anything.  Limits of all of them: M <= 32768, S <= 65536.  The workspaces are asked for with
+ * d = {N, M, 1, 1, 1, 1, 1, 0, 0}, the geometry of N rows.
+ *
+ * Norm by the root mean square of a row, with the residual's addition:
+ *   h = X + R (rounded to `dt`: the sum as it is held);   Y = rho h w,   rho = 1 / sqrt(mean_m h^2 + eps)
+ *   X       in   [N, M] element type `dt`
+ *   R       in   [N, M] element type `dt`, or NULL (h = X)
+ *   w       in   [M] float32, or NULL for all ones
+ *   eps     > 0
+ *   H       out  [N, M] element type `dt`: h, or NULL; may be X or R itself
+ *   Y       out  [N, M] element type `dt`, or NULL when q is given; overlaps nothing else
+ *   q, qs   out  [N, M] 8-bit integers and [N] float32, or both NULL: the same rows in 8 bits, Y ~ qs[n] q[n][m],
+ *                qs = max_m |rho h w| / 127, q = the nearest integer (ties to even) to rho h w / qs.  A row of zeros has qs = 0 and
+ *                q = 0, a row with an infinite or NaN entry has qs = NaN and q = 0.
+ * Sums in float64.
+ */
+fw_status fw_rms_norm(const void* X, const void* R, fw_dtype dt, int N, int M, const float* w, float eps, void* H, void* Y,
+                      signed char* q, float* qs, void* stream);
+
+/* Its gradient, from the row h as it was held:
+ *   dX = rho (w dY) - h rho^3 / M sum_m (w dY h) + dH,     dw = sum_n dY h rho
+ * dX is the gradient with respect to h, that is with respect to X and to R.
+ *   H       in   [N, M] element type `dt`: h (X, where there was no R)
+ *   dY      in   [N, M] element type `dt`
+ *   dH      in   [N, M] element type `dt`, the gradient that reaches h on the residual path, or NULL
+ *   dX      out  [N, M] element type `dt`; may be dY or dH itself, or NULL when dw is given
+ *   dw      out  [M] float32 (written, not added to), or NULL
+ *   ws      scratch, fw_workspace_bytes(FW_OP_RMS_NORM_GRAD, M, 0, d, dt) bytes, needed when dw is given
+ */
+fw_status fw_rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float* w, float eps, const void* dY, const void* dH,
+                           void* dX, float* dw, void* ws, size_t ws_bytes, void* stream);
+
+/* Gated feed-forward block: two projections of the same rows, an activation of one, their product:
+ *   g = X Wg^T + bg,   u = X Wu^T + bu,   H = act(g) u
+ * A layer that subtracts its input's mean, W (x - mu) + b, is run with the bias b - W mu (fw_bias_compensate gives it from mu_old =
+ * mu and mu_new = 0).
+ *   X       in   [N, M] element type `dt`
+ *   Wg, Wu  in   [S, M] element type `dt`
+ *   bg, bu  in   [S] float32, each may be NULL
+ *   H       out  [N, S] element type `dt`
+ *   Z       out  [2, N, S] element type `dt`, or NULL: what the backward pass needs of g and u, Z[0] = u act'(g) and Z[1] = act(g).
+ *                (These factors rather than g and u: one rounding to `dt` instead of the two of g and u reaches each gradient.)
+ *   ws      scratch, fw_workspace_bytes(FW_OP_GATED_FORWARD, M, S, d, dt) bytes
+ * Products and sums: FW_BF16 bfloat16 products summed in float32, FW_F32 float32 accuracy.  g, u, the activation and H before its
+ * rounding are float32.
+ */
+typedef enum {
+    FW_ACT_SILU = 0,       /* g / (1 + exp(-g)) */
+    FW_ACT_GELU = 1,       /* g (1 + erf(g / sqrt 2)) / 2 */
+    FW_ACT_GELU_TANH = 2,  /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+    FW_ACT_RELU = 3        /* max(g, 0), slope 0 at 0 */
+} fw_act;
+fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* bg,
+                           const float* bu, fw_act act, void* H, void* Z, void* ws, size_t ws_bytes, void* stream);
+
+/* Its gradient:  dg = dH Z[0],  du = dH Z[1],
+ *   dX = dg Wg + du Wu,    dWg = dg^T (X - 1 mu^T),  dWu = du^T (X - 1 mu^T),    dbg = sum_n dg,  dbu = sum_n du
+ * With mu the mean that the layer's whitening subtracts, dWg and dWu are the gradients G of Sec. 3.1 that fw_grad_transform and
+ * fw_sgd_update take (both projections have the same rows, hence the same Q).
+ *   X, Wg, Wu   in   as in the forward pass
+ *   Z           in   [2, N, S] element type `dt`, from the forward pass
+ *   dH          in   [N, S] element type `dt`
+ *   mu          in   [M] float32, or NULL for zero
+ *   dX          out  [N, M] element type `dt`, or NULL
+ *   dWg, dWu    out  [S, M] element type `dt`, or both NULL
+ *   dbg, dbu    out  [S] element type `dt`, or both NULL
+ *   ws          scratch, fw_workspace_bytes(FW_OP_GATED_GRAD, M, S, d, dt) bytes
+ * FW_BF16: dg and du are rounded to bfloat16 for the products, the sums are float32 and each result is rounded once.
+ */
+fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const void* Z,
+                        const void* dH, const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws,
+                        size_t ws_bytes, void* stream);
+
+/* Rows to 8 bits, each with its own scale: qs = max_m |X| / 127, q = the nearest integer (ties to even) to X / qs; zero and
+ * non-finite rows as in fw_rms_norm.  For activations a row is a token, for weights [S, M] a channel.
+ *   X  in [N, M] element type `dt`;   q out [N, M];   qs out [N] float32 */
+fw_status fw_int8_rows(const void* X, fw_dtype dt, int N, int M, signed char* q, float* qs, void* stream);
+
+/* Product of rows in 8 bits with weights in 8 bits:  Y[n][s] = sx[n] sw[s] sum_m Xq[n][m] Wq[s][m] + b[s]
+ *   Xq, sx  in   [N, M] 8-bit integers, [N] float32 scales of the tokens
+ *   Wq, sw  in   [S, M] 8-bit integers, [S] float32 scales of the channels
+ *   b       in   [S] float32, or NULL
+ *   Y       out  [N, S] element type `dt`
+ *   ws      scratch, fw_workspace_bytes(FW_OP_INT8_PRODUCT, M, S, d, dt) bytes (may be 0: then ws may be NULL)
+ * The sums are exact 32-bit integers (M <= 32768: below 2^30). */
+fw_status fw_int8_product(const signed char* Xq, const float* sx, int N, int M, int S, const signed char* Wq, const float* sw,
+                          const float* b, void* Y, fw_dtype dt, void* ws, size_t ws_bytes, void* stream);
+
 /* How fw_cov_accumulate would run a layer (host arithmetic only, no GPU call): for introspection and tests.
  *   shift              1: stride-1 window accumulated through shift correlations (tap pairs with the same offset share one
  *                      product), 0: direct products of the unfolded patch rows
@@ -382,8 +476,9 @@ fw_status fw_cov_plan_query(fw_dtype dt, fw_layout lay, const fw_conv_desc* d, f
  */
 fw_status fw_mfma_rate_probe(int zero_operands, int iters, float* sink, double* flops_host, void* stream);
 
-/* Scratch bytes an entry point needs for the given sizes (0 if none).  `d` is needed for FW_OP_COV_ACCUMULATE only;
- * for the per-tap operations S is the number of gradient rows, S * taps; for FW_OP_COND_PROBE S is the Krylov dimension k. */
+/* Scratch bytes an entry point needs for the given sizes (0 if none).  `d` is needed for FW_OP_COV_ACCUMULATE and the operations of (5);
+ * for the per-tap operations S is the number of gradient rows, S * taps; for FW_OP_COND_PROBE S is the Krylov dimension k; the operations
+ * of (5) take their number of rows N from d->B. */
 size_t fw_workspace_bytes(fw_op op, int M, int S, const fw_conv_desc* d, fw_dtype dt);
 
 const char* fw_status_string(fw_status st);

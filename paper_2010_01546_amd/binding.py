@@ -22,13 +22,16 @@ FW_OK, FW_ERR_INVALID_ARG, FW_ERR_UNSUPPORTED, FW_ERR_ALIGNMENT, FW_ERR_WORKSPAC
 FW_F32, FW_BF16 = 0, 1
 FW_LAYOUT_ROWS, FW_LAYOUT_NCHW, FW_LAYOUT_NHWC, FW_LAYOUT_NHWC_KKC = 0, 1, 2, 3
 (FW_OP_COV_ACCUMULATE, FW_OP_GRAD_TRANSFORM, FW_OP_COND_REDUCE_STEP, FW_OP_WHITEN_EVD, FW_OP_COND_STATE_REFRESH,
- FW_OP_GRAD_TRANSFORM_TAPS, FW_OP_SGD_UPDATE, FW_OP_DIAGNOSTICS, FW_OP_COND_PROBE) = range(9)
+ FW_OP_GRAD_TRANSFORM_TAPS, FW_OP_SGD_UPDATE, FW_OP_DIAGNOSTICS, FW_OP_COND_PROBE, FW_OP_RMS_NORM_GRAD, FW_OP_GATED_FORWARD,
+ FW_OP_GATED_GRAD, FW_OP_INT8_PRODUCT) = range(13)
+FW_ACT_SILU, FW_ACT_GELU, FW_ACT_GELU_TANH, FW_ACT_RELU = range(4)
 
 EXPORTS = ["fw_cov_accumulate", "fw_cov_finalize", "fw_grad_transform", "fw_cond_state_init", "fw_cond_reduce_step",
            "fw_whiten_evd", "fw_cond_state_refresh", "fw_grad_transform_taps", "fw_sgd_update", "fw_bias_compensate",
            "fw_diagnostics", "fw_cov_plan_query", "fw_cond_reduce_step_static", "fw_cond_probe", "fw_cond_refresh_plan_query",
-           "fw_grad_plan_query", "fw_mfma_rate_probe", "fw_workspace_bytes", "fw_status_string", "fw_version"]
-N_STATUS_EXPORTS = 17   # the leading entries of EXPORTS return fw_status
+           "fw_grad_plan_query", "fw_mfma_rate_probe", "fw_rms_norm", "fw_rms_norm_grad", "fw_gated_forward", "fw_gated_grad",
+           "fw_int8_rows", "fw_int8_product", "fw_workspace_bytes", "fw_status_string", "fw_version"]
+N_STATUS_EXPORTS = 23   # the leading entries of EXPORTS return fw_status
 
 
 class fw_conv_desc(C.Structure):
@@ -90,6 +93,12 @@ lib.fw_cond_refresh_plan_query.argtypes = [C.c_int, C.c_size_t, C.POINTER(fw_ref
 lib.fw_cov_plan_query.argtypes = [C.c_int, C.c_int, C.POINTER(fw_conv_desc), C.POINTER(fw_cov_plan)]
 lib.fw_grad_plan_query.argtypes = [C.c_int, C.c_int, C.c_int, C.c_size_t, C.POINTER(fw_grad_plan)]
 lib.fw_mfma_rate_probe.argtypes = [C.c_int, C.c_int, _P, C.POINTER(C.c_double), _P]
+lib.fw_rms_norm.argtypes = [_P, _P, C.c_int, C.c_int, C.c_int, _P, C.c_float, _P, _P, _P, _P, _P]
+lib.fw_rms_norm_grad.argtypes = [_P, C.c_int, C.c_int, C.c_int, _P, C.c_float, _P, _P, _P, _P, _P, C.c_size_t, _P]
+lib.fw_gated_forward.argtypes = [_P, C.c_int, C.c_int, C.c_int, C.c_int, _P, _P, _P, _P, C.c_int, _P, _P, _P, C.c_size_t, _P]
+lib.fw_gated_grad.argtypes = [_P, C.c_int, C.c_int, C.c_int, C.c_int, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]
+lib.fw_int8_rows.argtypes = [_P, C.c_int, C.c_int, C.c_int, _P, _P, _P]
+lib.fw_int8_product.argtypes = [_P, _P, C.c_int, C.c_int, C.c_int, _P, _P, _P, _P, C.c_int, _P, C.c_size_t, _P]
 lib.fw_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(fw_conv_desc), C.c_int]
 lib.fw_workspace_bytes.restype = C.c_size_t
 lib.fw_status_string.argtypes = [C.c_int]
@@ -196,6 +205,39 @@ def fw_bias_compensate(b, W, S, M, taps, mu_old, mu_new, scale=1.0, stream=None)
 def fw_diagnostics(Phi_y, lam, M, out, ws=None, stream=None):
     wp, n = _ws(ws)
     return _check(lib.fw_diagnostics(_ptr(Phi_y), _ptr(lam), M, _ptr(out), wp, n, _stream(stream)), "fw_diagnostics")
+
+
+def fw_rms_norm(X, R, dt, N, M, w, eps, H, Y, q=None, qs=None, stream=None):
+    return _check(lib.fw_rms_norm(_ptr(X), _ptr(R), dt, N, M, _ptr(w), float(eps), _ptr(H), _ptr(Y), _ptr(q), _ptr(qs), _stream(stream)),
+                  "fw_rms_norm")
+
+
+def fw_rms_norm_grad(H, dt, N, M, w, eps, dY, dH, dX, dw, ws=None, stream=None):
+    p, n = _ws(ws)
+    return _check(lib.fw_rms_norm_grad(_ptr(H), dt, N, M, _ptr(w), float(eps), _ptr(dY), _ptr(dH), _ptr(dX), _ptr(dw), p, n,
+                                       _stream(stream)), "fw_rms_norm_grad")
+
+
+def fw_gated_forward(X, dt, N, M, S, Wg, Wu, bg, bu, act, H, Z=None, ws=None, stream=None):
+    p, n = _ws(ws)
+    return _check(lib.fw_gated_forward(_ptr(X), dt, N, M, S, _ptr(Wg), _ptr(Wu), _ptr(bg), _ptr(bu), act, _ptr(H), _ptr(Z), p, n,
+                                       _stream(stream)), "fw_gated_forward")
+
+
+def fw_gated_grad(X, dt, N, M, S, Wg, Wu, Z, dH, mu, dX, dWg, dWu, dbg=None, dbu=None, ws=None, stream=None):
+    p, n = _ws(ws)
+    return _check(lib.fw_gated_grad(_ptr(X), dt, N, M, S, _ptr(Wg), _ptr(Wu), _ptr(Z), _ptr(dH), _ptr(mu), _ptr(dX), _ptr(dWg), _ptr(dWu),
+                                    _ptr(dbg), _ptr(dbu), p, n, _stream(stream)), "fw_gated_grad")
+
+
+def fw_int8_rows(X, dt, N, M, q, qs, stream=None):
+    return _check(lib.fw_int8_rows(_ptr(X), dt, N, M, _ptr(q), _ptr(qs), _stream(stream)), "fw_int8_rows")
+
+
+def fw_int8_product(Xq, sx, N, M, S, Wq, sw, b, Y, dt, ws=None, stream=None):
+    p, n = _ws(ws)
+    return _check(lib.fw_int8_product(_ptr(Xq), _ptr(sx), N, M, S, _ptr(Wq), _ptr(sw), _ptr(b), _ptr(Y), dt, p, n, _stream(stream)),
+                  "fw_int8_product")
 
 
 FW_COND_PROBE_MAX_K = 32

@@ -58,6 +58,14 @@ fw_status split_rows_apply(const float* rows, int n, int M, const float* Q, cons
     return grad_epilogue_from_runs(sp, runs, e, n, M, st);
 }
 
+// sizes that the layers of language models take
+fw_status rows_check(fw_dtype dt, int N, int M, int S) {
+    if (N <= 0 || M <= 0 || S <= 0 || !dtype_ok(dt)) return FW_ERR_INVALID_ARG;
+    return M > 32768 || S > 65536 ? FW_ERR_UNSUPPORTED : FW_OK;
+}
+template <class... P>
+bool all_aligned16(const P*... p) { return (aligned16(p) && ...); }
+
 }  // namespace
 
 extern "C" {
@@ -304,6 +312,68 @@ fw_status fw_whiten_evd(const float* Phi_x, int M, const fw_evd_params* p, float
     return whiten_evd(Phi_x, M, p, T, Q, Qs, lambda, ws, ws_bytes, reinterpret_cast<hipStream_t>(stream));
 }
 
+fw_status fw_rms_norm(const void* X, const void* R, fw_dtype dt, int N, int M, const float* w, float eps, void* H, void* Y, signed char* q,
+                      float* qs, void* stream) {
+    if (!X || (!Y && !q) || !q != !qs || !(eps > 0.f) || (Y && (Y == X || Y == R || Y == H))) return FW_ERR_INVALID_ARG;
+    const fw_status rc = rows_check(dt, N, M, 1);
+    if (rc != FW_OK) return rc;
+    if (!all_aligned16(X, R, w, H, Y, q, qs)) return FW_ERR_ALIGNMENT;
+    return rms_norm(X, R, dt, N, M, w, eps, H, Y, q, qs, reinterpret_cast<hipStream_t>(stream));
+}
+
+fw_status fw_rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float* w, float eps, const void* dY, const void* dH, void* dX,
+                           float* dw, void* ws, size_t ws_bytes, void* stream) {
+    if (!H || !dY || (!dX && !dw) || !(eps > 0.f) || dX == H) return FW_ERR_INVALID_ARG;
+    const fw_status rc = rows_check(dt, N, M, 1);
+    if (rc != FW_OK) return rc;
+    if (!all_aligned16(H, w, dY, dH, dX, dw, ws)) return FW_ERR_ALIGNMENT;
+    if (dw && (!ws || ws_bytes < rms_norm_grad_workspace_bytes(N, M))) return FW_ERR_WORKSPACE;
+    return rms_norm_grad(H, dt, N, M, w, eps, dY, dH, dX, dw, ws, reinterpret_cast<hipStream_t>(stream));
+}
+
+fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu,
+                           fw_act act, void* H, void* Z, void* ws, size_t ws_bytes, void* stream) {
+    if (!X || !Wg || !Wu || !H || (int)act < FW_ACT_SILU || (int)act > FW_ACT_RELU || H == X || H == Z || (Z && Z == X)) return FW_ERR_INVALID_ARG;
+    const fw_status rc = rows_check(dt, N, M, S);
+    if (rc != FW_OK) return rc;
+    if (!all_aligned16(X, Wg, Wu, bg, bu, H, Z, ws)) return FW_ERR_ALIGNMENT;
+    const size_t need = gated_forward_workspace_bytes(dt, N, M, S);
+    if (need && (!ws || ws_bytes < need)) return FW_ERR_WORKSPACE;
+    return gated_forward(X, dt, N, M, S, Wg, Wu, bg, bu, act, H, Z, ws, reinterpret_cast<hipStream_t>(stream));
+}
+
+fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const void* Z, const void* dH,
+                        const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws, size_t ws_bytes, void* stream) {
+    if (!X || !Wg || !Wu || !Z || !dH || !dWg != !dWu || !dbg != !dbu || (!dX && !dWg && !dbg)) return FW_ERR_INVALID_ARG;
+    if (dX && (dX == X || dX == dH || dX == Z)) return FW_ERR_INVALID_ARG;
+    if (dWg && (dWg == dWu || dWg == Wg || dWg == Wu || dWu == Wg || dWu == Wu)) return FW_ERR_INVALID_ARG;
+    if (dbg && dbg == dbu) return FW_ERR_INVALID_ARG;
+    const fw_status rc = rows_check(dt, N, M, S);
+    if (rc != FW_OK) return rc;
+    if (!all_aligned16(X, Wg, Wu, Z, dH, mu, dX, dWg, dWu, dbg, dbu, ws)) return FW_ERR_ALIGNMENT;
+    if (!ws || ws_bytes < gated_grad_workspace_bytes(dt, N, M, S)) return FW_ERR_WORKSPACE;
+    return gated_grad(X, dt, N, M, S, Wg, Wu, Z, dH, mu, dX, dWg, dWu, dbg, dbu, ws, reinterpret_cast<hipStream_t>(stream));
+}
+
+fw_status fw_int8_rows(const void* X, fw_dtype dt, int N, int M, signed char* q, float* qs, void* stream) {
+    if (!X || !q || !qs || X == (const void*)q) return FW_ERR_INVALID_ARG;
+    const fw_status rc = rows_check(dt, N, M, 1);
+    if (rc != FW_OK) return rc;
+    if (!all_aligned16(X, q, qs)) return FW_ERR_ALIGNMENT;
+    return int8_rows(X, dt, N, M, q, qs, reinterpret_cast<hipStream_t>(stream));
+}
+
+fw_status fw_int8_product(const signed char* Xq, const float* sx, int N, int M, int S, const signed char* Wq, const float* sw, const float* b,
+                          void* Y, fw_dtype dt, void* ws, size_t ws_bytes, void* stream) {
+    if (!Xq || !sx || !Wq || !sw || !Y || Y == (const void*)Xq || Y == (const void*)Wq) return FW_ERR_INVALID_ARG;
+    const fw_status rc = rows_check(dt, N, M, S);
+    if (rc != FW_OK) return rc;
+    if (!all_aligned16(Xq, sx, Wq, sw, b, Y, ws)) return FW_ERR_ALIGNMENT;
+    const size_t need = int8_product_workspace_bytes(N, M, S);
+    if (need && (!ws || ws_bytes < need)) return FW_ERR_WORKSPACE;
+    return int8_product(Xq, sx, N, M, S, Wq, sw, b, Y, dt, ws, reinterpret_cast<hipStream_t>(stream));
+}
+
 fw_status fw_cov_plan_query(fw_dtype dt, fw_layout lay, const fw_conv_desc* d, fw_cov_plan* plan) {
     if (!plan || !d || !dtype_ok(dt) || !layout_ok(lay) || !desc_ok(d, lay)) return FW_ERR_INVALID_ARG;
     return cov_plan(d, dt, lay, plan) ? FW_OK : FW_ERR_UNSUPPORTED;
@@ -331,6 +401,10 @@ size_t fw_workspace_bytes(fw_op op, int M, int S, const fw_conv_desc* d, fw_dtyp
         case FW_OP_COND_STATE_REFRESH: return M > 0 && M <= 16384 ? cond_refresh_workspace_bytes(M) : 0;
         case FW_OP_GRAD_TRANSFORM_TAPS:
         case FW_OP_SGD_UPDATE: return (M > 0 && M <= 16384 && S > 0) ? grad_wide_bytes(S, M) + grad_split_bytes(S, M) : 0;
+        case FW_OP_RMS_NORM_GRAD: return d && rows_check(dt, d->B, M, 1) == FW_OK ? rms_norm_grad_workspace_bytes(d->B, M) : 0;
+        case FW_OP_GATED_FORWARD: return d && rows_check(dt, d->B, M, S) == FW_OK ? gated_forward_workspace_bytes(dt, d->B, M, S) : 0;
+        case FW_OP_GATED_GRAD: return d && rows_check(dt, d->B, M, S) == FW_OK ? gated_grad_workspace_bytes(dt, d->B, M, S) : 0;
+        case FW_OP_INT8_PRODUCT: return d && rows_check(dt, d->B, M, S) == FW_OK ? int8_product_workspace_bytes(d->B, M, S) : 0;
         case FW_OP_DIAGNOSTICS: return M > 0 && M <= 16384 ? diagnostics_workspace_bytes(M) : 0;
         case FW_OP_COND_PROBE: return M > 0 && M <= 16384 ? cond_probe_workspace_bytes(M, S > 0 ? S : FW_COND_PROBE_MAX_K) : 0;
     }

@@ -187,6 +187,27 @@ fw_status diagnostics(const float* Phi_y, const float* lambda, int M, float* out
 size_t cond_probe_workspace_bytes(int M, int k);
 fw_status cond_probe(const float* Phi_y, int M, const float* b0, int k, float* out, void* ws, hipStream_t st);
 
+// ---- norm.hip
+size_t rms_norm_grad_workspace_bytes(int N, int M);
+fw_status rms_norm(const void* X, const void* R, fw_dtype dt, int N, int M, const float* w, float eps, void* H, void* Y, signed char* q,
+                   float* qs, hipStream_t st);
+fw_status rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float* w, float eps, const void* dY, const void* dH, void* dX,
+                        float* dw, void* ws, hipStream_t st);
+fw_status int8_rows(const void* X, fw_dtype dt, int N, int M, signed char* q, float* qs, hipStream_t st);
+
+// ---- gated.hip
+size_t gated_forward_workspace_bytes(fw_dtype dt, int N, int M, int S);
+size_t gated_grad_workspace_bytes(fw_dtype dt, int N, int M, int S);
+fw_status gated_forward(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu,
+                        fw_act act, void* H, void* Z, void* ws, hipStream_t st);
+fw_status gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const void* Z, const void* dH,
+                     const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws, hipStream_t st);
+
+// ---- int8.hip
+size_t int8_product_workspace_bytes(int N, int M, int S);
+fw_status int8_product(const signed char* Xq, const float* sx, int N, int M, int S, const signed char* Wq, const float* sw, const float* b,
+                       void* Y, fw_dtype dt, void* ws, hipStream_t st);
+
 // ---- cond.hip
 size_t cond_workspace_bytes(int M);
 fw_status cond_state_init(const fw_cond_state* s, hipStream_t st);

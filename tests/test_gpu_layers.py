@@ -1,0 +1,425 @@
+"""GPU parity of the layers around the whitening (norm, gated block, 8-bit product) against the float64 oracle.
+
+Tolerances: U32 = 2^-24 and half(t) (2^-8 for bfloat16, 2^-24 for float32) are the most a rounding is off by, relative to its value; a
+float32 sum of K terms in any order is off by at most (K + a few) U32 times the sum of the terms' magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+import workloads as wl
+from gpu_common import DEV, b, dev, relF, workspace
+from oracle import layer_oracle as lo
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+TDT = {"f32": torch.float32, "bf16": torch.bfloat16}
+FDT = {"f32": b.FW_F32, "bf16": b.FW_BF16}
+EPS = 1e-5
+
+
+def rows(rng, n, m, dtype, scale=1.0):
+    x = (scale * rng.standard_normal((n, m)) * np.exp(0.5 * rng.standard_normal(m))).astype(np.float32)
+    return wl.round_to_bf16(x) if dtype == "bf16" else x
+
+
+class Out:
+    """An output with a guard behind it that no call may touch."""
+    GUARD = 96
+
+    def __init__(self, *shape, dtype):
+        n = int(np.prod(shape))
+        self.fill = 77 if dtype == torch.int8 else float("nan")
+        self.buf = torch.full((n + self.GUARD,), self.fill, dtype=dtype, device=DEV)
+        self.t = self.buf[:n].view(*shape)
+
+    def host(self):
+        tail = self.buf[self.t.numel():].float()
+        assert bool((tail == 77).all() if self.fill == 77 else torch.isnan(tail).all()), "written behind the end"
+        return self.t.float().cpu().numpy().astype(np.float64)
+
+
+def within(got, want, tol, what=""):
+    assert got.shape == want.shape, what
+    bad = ~(np.abs(got - want) <= tol)
+    if bad.any():
+        i = tuple(np.argwhere(bad)[0])
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.size} off, first at {i}: {got[i]!r} for {want[i]!r}, allowed {np.broadcast_to(tol, got.shape)[i]:.3g}")
+
+
+# ---------------------------------------------------------------------------------------------------------------- norm
+
+NORM_SIZES = [(1, 1), (1, 7), (2, 8), (3, 64), (5, 129), (4, 512), (7, 513), (3, 1025), (6, 2048), (2, 2049), (1, 4608), (3, 8192), (2, 8197),
+              (2, 16384), (1, 16391), (2, 32768), (65, 48), (1030, 72), (4101, 33)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M", NORM_SIZES)
+def test_norm(N, M, dtype):
+    rng = np.random.default_rng(N * 100003 + M)
+    t, dt = TDT[dtype], FDT[dtype]
+    X, R = rows(rng, N, M, dtype), rows(rng, N, M, dtype, 2.0)
+    w = (1 + 0.2 * rng.standard_normal(M)).astype(np.float32)
+    Xd, Rd = dev(X, t), dev(R, t)
+    H, Y, q, qs = Out(N, M, dtype=t), Out(N, M, dtype=t), Out(N, M, dtype=torch.int8), Out(N, dtype=torch.float32)
+    b.fw_rms_norm(Xd, Rd, dt, N, M, dev(w), EPS, H.t, Y.t, q.t, qs.t)
+    torch.cuda.synchronize()
+    held = (Xd.float() + Rd.float()).to(t)
+    assert torch.equal(H.t, held)
+    h = held.float().cpu().numpy().astype(np.float64)
+    want = lo.rms_norm(h, w, EPS)
+    within(Y.host(), want, np.abs(want) * (HALF[dtype] + 4 * U32), "Y")          # rho, two products, the last rounding
+    steps, s = lo.int8_steps(want)
+    within(q.host(), steps, 0.5 + 1e-9, "q")
+    within(qs.host(), s, s * 1.01 * U32, "qs")
+    # without the residual, without w, 8 bits alone and 16 or 32 bits alone: each its own call
+    Y2, q2, qs2 = Out(N, M, dtype=t), Out(N, M, dtype=torch.int8), Out(N, dtype=torch.float32)
+    b.fw_rms_norm(held, None, dt, N, M, None, EPS, None, Y2.t)
+    b.fw_rms_norm(held, None, dt, N, M, dev(w), EPS, None, None, q2.t, qs2.t)
+    torch.cuda.synchronize()
+    want = lo.rms_norm(h, None, EPS)
+    within(Y2.host(), want, np.abs(want) * (HALF[dtype] + 4 * U32), "Y without w")
+    assert torch.equal(q2.t, q.t) and torch.equal(qs2.t, qs.t)
+    q2.host(), qs2.host()
+    # the sum in place of either addend
+    X2, R2 = Xd.clone(), Rd.clone()
+    b.fw_rms_norm(X2, Rd, dt, N, M, dev(w), EPS, X2, Y2.t)
+    torch.cuda.synchronize()
+    assert torch.equal(X2, held) and torch.equal(Y2.t, Y.t)
+    b.fw_rms_norm(Xd, R2, dt, N, M, dev(w), EPS, R2, Y2.t)
+    torch.cuda.synchronize()
+    assert torch.equal(R2, held) and torch.equal(Y2.t, Y.t)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M", NORM_SIZES)
+def test_norm_gradient(N, M, dtype):
+    rng = np.random.default_rng(N * 100019 + M)
+    t, dt = TDT[dtype], FDT[dtype]
+    Hh, dY, dHh = rows(rng, N, M, dtype), rows(rng, N, M, dtype, 0.1), rows(rng, N, M, dtype, 0.1)
+    w = (1 + 0.2 * rng.standard_normal(M)).astype(np.float32)
+    Hd, dYd, dHd, wd = dev(Hh, t), dev(dY, t), dev(dHh, t), dev(w)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_RMS_NORM_GRAD, M, 0, b.conv_desc(N, M), dt))
+    dX, dw = Out(N, M, dtype=t), Out(M, dtype=torch.float32)
+    b.fw_rms_norm_grad(Hd, dt, N, M, wd, EPS, dYd, dHd, dX.t, dw.t, ws)
+    torch.cuda.synchronize()
+    want, want_w = lo.rms_norm_grad(Hh, w, EPS, dY, dHh)
+    rho = 1 / np.sqrt(np.mean(lo.f64(Hh) ** 2, axis=1, keepdims=True) + EPS)
+    first = np.abs(rho * lo.f64(dY) * w)
+    second = np.abs(Hh * rho ** 3 * np.mean(lo.f64(dY) * w * Hh, axis=1, keepdims=True))
+    within(dX.host(), want, np.abs(want) * HALF[dtype] + 5 * U32 * (first + second + np.abs(dHh)), "dX")
+    terms = np.abs(lo.f64(dY) * Hh * rho)
+    within(dw.host(), want_w, (min(N, 100 + N // 1024) + 4) * U32 * terms.sum(0), "dw")   # chains: a workgroup's rows, a slice, the slices
+    # one output at a time, no residual path, no w, in place of dY and of dH
+    dX2, dw2 = Out(N, M, dtype=t), Out(M, dtype=torch.float32)
+    b.fw_rms_norm_grad(Hd, dt, N, M, wd, EPS, dYd, dHd, dX2.t, None)
+    b.fw_rms_norm_grad(Hd, dt, N, M, wd, EPS, dYd, None, None, dw2.t, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(dX2.t, dX.t) and torch.equal(dw2.t, dw.t)
+    for src in ("dY", "dH"):
+        a, c = dYd.clone(), dHd.clone()
+        b.fw_rms_norm_grad(Hd, dt, N, M, wd, EPS, a, c, a if src == "dY" else c, dw2.t, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(a if src == "dY" else c, dX.t) and torch.equal(dw2.t, dw.t)
+    b.fw_rms_norm_grad(Hd, dt, N, M, None, EPS, dYd, None, dX2.t, None)
+    torch.cuda.synchronize()
+    want = lo.rms_norm_grad(Hh, None, EPS, dY)[0]
+    first, second = np.abs(rho * lo.f64(dY)), np.abs(Hh * rho ** 3 * np.mean(lo.f64(dY) * Hh, axis=1, keepdims=True))
+    within(dX2.host(), want, np.abs(want) * HALF[dtype] + 5 * U32 * (first + second), "dX without w")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_of_extreme_rows(dtype):
+    t, dt, M = TDT[dtype], FDT[dtype], 70
+    X = np.ones((8, M), dtype=np.float32)
+    X[0] = 0.0
+    X[1] *= 1e30             # squares beyond float32
+    X[2] *= 1e-30
+    X[3, 5] = np.inf
+    X[4, 69] = np.nan
+    X[5, :] = -3.0
+    X[6, 1:] = 0.0
+    X[7, 0] = 250.0
+    X = wl.round_to_bf16(X) if dtype == "bf16" else X
+    Y, q, qs = Out(8, M, dtype=t), Out(8, M, dtype=torch.int8), Out(8, dtype=torch.float32)
+    b.fw_rms_norm(dev(X, t), None, dt, 8, M, None, EPS, None, Y.t, q.t, qs.t)
+    q3, qs3 = Out(8, M, dtype=torch.int8), Out(8, dtype=torch.float32)
+    b.fw_int8_rows(dev(X, t), dt, 8, M, q3.t, qs3.t)
+    torch.cuda.synchronize()
+    fine = [0, 1, 2, 5, 6, 7]
+    want = lo.rms_norm(X[fine], None, EPS)
+    within(Y.host()[fine], want, np.abs(want) * (HALF[dtype] + 4 * U32))
+    for got, scale, src in ((q.host(), qs.host(), want), (q3.host(), qs3.host(), lo.f64(X[fine]))):
+        steps, s = lo.int8_steps(src)
+        within(got[fine], steps, 0.5 + 1e-9)
+        within(scale[fine], s, s * 1.01 * U32)
+        assert scale[0] == 0 and np.isnan(scale[[3, 4]]).all() and not got[[0, 3, 4]].any()
+    assert np.isnan(Y.host()[3, 5]) and np.isnan(Y.host()[4]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M", [(1, 1), (3, 9), (17, 64), (5, 1000), (2, 2305), (1, 12288), (2, 32768), (300, 576)])
+def test_int8_rows(N, M, dtype):
+    rng = np.random.default_rng(N + M)
+    X = rows(rng, N, M, dtype)
+    q, qs = Out(N, M, dtype=torch.int8), Out(N, dtype=torch.float32)
+    b.fw_int8_rows(dev(X, TDT[dtype]), FDT[dtype], N, M, q.t, qs.t)
+    torch.cuda.synchronize()
+    steps, s = lo.int8_steps(X)
+    within(q.host(), steps, 0.5 + 1e-9)
+    within(qs.host(), s, s * 1.01 * U32)
+    assert np.abs(q.host()).max() == 127
+
+
+# --------------------------------------------------------------------------------------------------------- gated block
+
+GATED_SIZES = [(1, 1, 1), (1, 8, 5), (1, 64, 128), (2, 33, 65), (3, 130, 64), (7, 256, 200), (16, 576, 96), (17, 72, 257), (31, 1000, 33),
+               (32, 512, 512), (33, 40, 130), (64, 64, 64), (65, 96, 129), (127, 129, 513), (128, 576, 256), (130, 200, 1000), (200, 1153, 67),
+               (257, 320, 384), (300, 72, 700), (513, 257, 300), (1100, 64, 72), (1, 2304, 300), (4, 4608, 40), (520, 513, 1030)]
+ACT = {k: i for i, k in enumerate(lo.ACTS)}
+
+
+def act_of(N, M, S):
+    return lo.ACTS[(N + M + S) % 4]
+
+
+def gated_inputs(N, M, S, dtype, bias):
+    rng = np.random.default_rng(N * 7919 + M * 31 + S)
+    X = rows(rng, N, M, dtype)
+    Wg, Wu = (rows(rng, S, M, dtype, M ** -0.5) for _ in range(2))
+    bg, bu = ((0.3 * rng.standard_normal(S)).astype(np.float32) if bias else None for _ in range(2))
+    return rng, X, Wg, Wu, bg, bu
+
+
+def run_forward(X, Wg, Wu, bg, bu, kind, dtype, keep=True):
+    (N, M), S, t = X.shape, Wg.shape[0], TDT[dtype]
+    H, Z = Out(N, S, dtype=t), Out(2, N, S, dtype=t) if keep else None
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_FORWARD, M, S, b.conv_desc(N, M), FDT[dtype]))
+    ws.fill_(255)
+    b.fw_gated_forward(dev(X, t), FDT[dtype], N, M, S, dev(Wg, t), dev(Wu, t), None if bg is None else dev(bg), None if bu is None else dev(bu),
+                       ACT[kind], H.t, Z.t if keep else None, ws)
+    torch.cuda.synchronize()
+    return H, Z
+
+
+def check_forward(H, Z, X, Wg, Wu, bg, bu, kind, dtype):
+    M = X.shape[1]
+    g, u = lo.projections(X, Wg, Wu, bg, bu)
+    mag = lambda W, c: np.abs(lo.f64(X)) @ np.abs(lo.f64(W)).T + (0 if c is None else np.abs(c))  # noqa: E731
+    eg, eu = (M + 8) * U32 * mag(Wg, bg), (M + 8) * U32 * mag(Wu, bu)
+    a, da = lo.act(kind, g), lo.act_slope(kind, g)
+    # |act'| <= 1.13 for all of them, act evaluated to a few units of float32 of max(|g|, 1)
+    tol = 1.2 * eg * (np.abs(u) + eu) + np.abs(a) * eu + 16 * U32 * np.abs(g * u)
+    within(H, a * u, tol + np.abs(a * u) * HALF[dtype] + 1e-38, "H")
+    if Z is None:
+        return
+    # |act''| <= 1.2; the slope of relu is that of a g on the same side of zero
+    sure = np.abs(g) > eg if kind == "relu" else np.ones_like(g, dtype=bool)
+    tol = np.abs(u) * 1.2 * eg + 1.2 * eu + 16 * U32 * (1 + np.abs(g)) * np.abs(u)
+    within(np.where(sure, Z[0], 0), np.where(sure, u * da, 0), tol + np.abs(u * da) * HALF[dtype] + 1e-38, "Z[0]")
+    within(Z[1], a, 1.2 * eg + 16 * U32 * np.abs(g) + np.abs(a) * HALF[dtype] + 1e-38, "Z[1]")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M,S", GATED_SIZES)
+def test_gated_forward(N, M, S, dtype):
+    kind, bias = act_of(N, M, S), (N + S) % 3 != 0
+    _, X, Wg, Wu, bg, bu = gated_inputs(N, M, S, dtype, bias)
+    H, Z = run_forward(X, Wg, Wu, bg, bu, kind, dtype)
+    check_forward(H.host(), Z.host(), X, Wg, Wu, bg, bu, kind, dtype)
+    H2, _ = run_forward(X, Wg, Wu, bg, bu, kind, dtype, keep=False)
+    assert torch.equal(H2.t, H.t)
+    H2.host()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", lo.ACTS)
+@pytest.mark.parametrize("N", [1, 70])
+def test_gated_activations(N, kind, dtype):
+    _, X, Wg, Wu, bg, _ = gated_inputs(N, 72, 100, dtype, True)
+    H, Z = run_forward(4 * X, Wg, Wu, bg, None, kind, dtype)
+    check_forward(H.host(), Z.host(), 4 * X, Wg, Wu, bg, None, kind, dtype)
+
+
+def rounded_product(a, c, dtype):
+    """dH times a factor as the block's gradient has it: exact in float32 for bfloat16 factors, rounded once to the type."""
+    p = (lo.f64(a) * c).astype(np.float32)
+    return lo.f64(wl.round_to_bf16(p) if dtype == "bf16" else p)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M,S", GATED_SIZES)
+def test_gated_gradient(N, M, S, dtype):
+    kind, bias, t, dt = act_of(N, M, S), (N + S) % 3 != 0, TDT[dtype], FDT[dtype]
+    rng, X, Wg, Wu, bg, bu = gated_inputs(N, M, S, dtype, bias)
+    dH = rows(rng, N, S, dtype, 0.1)
+    mu = lo.f64(X).mean(0).astype(np.float32) + 0.1 if (N + M) % 2 else None
+    _, Z = run_forward(X, Wg, Wu, bg, bu, kind, dtype)
+    Zh = Z.host()
+    dX, dWg, dWu, dbg, dbu = Out(N, M, dtype=t), Out(S, M, dtype=t), Out(S, M, dtype=t), Out(S, dtype=t), Out(S, dtype=t)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_GRAD, M, S, b.conv_desc(N, M), dt))
+    ws.fill_(255)                                                  # NaN in every type: nothing may be read before it is written
+    Xd, Wgd, Wud, dHd, mud = dev(X, t), dev(Wg, t), dev(Wu, t), dev(dH, t), None if mu is None else dev(mu)
+    b.fw_gated_grad(Xd, dt, N, M, S, Wgd, Wud, Z.t, dHd, mud, dX.t, dWg.t, dWu.t, dbg.t, dbu.t, ws)
+    torch.cuda.synchronize()
+    dg, du = rounded_product(dH, Zh[0], dtype), rounded_product(dH, Zh[1], dtype)
+    half = HALF[dtype]
+    want = lo.gated_grad_from(dg, du, X, Wg, Wu, mu)
+    ag, au, aX = np.abs(dg), np.abs(du), np.abs(lo.f64(X)) + (0 if mu is None else np.abs(mu))
+    more = U32 if dtype == "f32" else 0.0                           # float32: the rounding of dg and du themselves
+    within(dX.host(), want[0], ((2 * S + 8) * U32 + more) * (ag @ np.abs(lo.f64(Wg)) + au @ np.abs(lo.f64(Wu))) + half * np.abs(want[0]), "dX")
+    within(dWg.host(), want[1], ((2 * N + 8) * U32 + more) * (ag.T @ aX) + half * np.abs(want[1]), "dWg")
+    within(dWu.host(), want[2], ((2 * N + 8) * U32 + more) * (au.T @ aX) + half * np.abs(want[2]), "dWu")
+    within(dbg.host(), want[3], ((N + 4) * U32 + more) * ag.sum(0) + half * np.abs(want[3]), "dbg")
+    within(dbu.host(), want[4], ((N + 4) * U32 + more) * au.sum(0) + half * np.abs(want[4]), "dbu")
+    # against the whole formula in 64 bits: the factors, dg and du, and the results have a rounding each, independent of each other
+    # (random-sign model: 3 of at most `half`); float32 adds its sums
+    full = lo.gated_grad(X, Wg, Wu, kind, dH, bg, bu, mu)
+    if kind != "relu":
+        for got, w, what in zip((dX, dWg, dWu), full, ("dX", "dWg", "dWu")):
+            assert relF(got.host(), w) < (3 * half if dtype == "bf16" else 2e-5), what
+    # one group of outputs at a time
+    alone = [Out(N, M, dtype=t), Out(S, M, dtype=t), Out(S, M, dtype=t), Out(S, dtype=t), Out(S, dtype=t)]
+    b.fw_gated_grad(Xd, dt, N, M, S, Wgd, Wud, Z.t, dHd, None, alone[0].t, None, None, None, None, ws)
+    b.fw_gated_grad(Xd, dt, N, M, S, Wgd, Wud, Z.t, dHd, mud, None, alone[1].t, alone[2].t, None, None, ws)
+    b.fw_gated_grad(Xd, dt, N, M, S, Wgd, Wud, Z.t, dHd, None, None, None, None, alone[3].t, alone[4].t, ws)
+    torch.cuda.synchronize()
+    for a, c in zip(alone, (dX, dWg, dWu, dbg, dbu)):
+        assert torch.equal(a.t, c.t)
+        a.host()
+
+
+# -------------------------------------------------------------------------------------------------------- 8-bit product
+
+INT8_SIZES = [(1, 1, 1), (1, 16, 5), (1, 4608, 100), (2, 33, 65), (3, 130, 64), (7, 1000, 200), (16, 576, 96), (17, 72, 257), (32, 512, 512), (33, 48, 130),
+              (64, 64, 64), (65, 97, 129), (128, 576, 256), (130, 208, 1000), (257, 320, 384), (513, 257, 300), (1100, 64, 72), (5, 32768, 9), (300, 1153, 520)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M,S", INT8_SIZES)
+def test_int8_product(N, M, S, dtype):
+    rng = np.random.default_rng(N + 13 * M + 7 * S)
+    Xq = rng.integers(-128, 128, (N, M)).astype(np.int8)
+    Wq = rng.integers(-128, 128, (S, M)).astype(np.int8)
+    if N == 5:
+        Xq[0], Wq[0], Wq[1] = -128, -128, 127                      # the largest sums there are
+    sx, sw = (np.exp(rng.standard_normal(n)).astype(np.float32) * 1e-2 for n in (N, S))
+    sx[0] = 0.0 if N > 2 and N != 5 else sx[0]
+    bias = rng.standard_normal(S).astype(np.float32) if (N + S) % 2 else None
+    Y = Out(N, S, dtype=TDT[dtype])
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_INT8_PRODUCT, M, S, b.conv_desc(N, M), FDT[dtype]))
+    ws.fill_(255)
+    b.fw_int8_product(dev(Xq, torch.int8), dev(sx), N, M, S, dev(Wq, torch.int8), dev(sw), None if bias is None else dev(bias), Y.t, FDT[dtype], ws)
+    torch.cuda.synchronize()
+    want = lo.int8_product(Xq, sx, Wq, sw, bias)
+    plain = np.abs(lo.int8_product(Xq, sx, Wq, sw))
+    within(Y.host(), want, 4 * U32 * (plain + (0 if bias is None else np.abs(bias))) + HALF[dtype] * np.abs(want))
+
+
+# -------------------------------------------------------------------------------------------- as they are used together
+
+def whitened_step(dtype, stream=None):
+    """Residual and norm, gated block, its gradient with the centred rows, the norm's gradient; then the whitening's own calls on the
+    block's input rows and weight gradients.  Returns host arrays of everything."""
+    N, M, S, t, dt = 192, 64, 160, TDT[dtype], FDT[dtype]
+    rng = np.random.default_rng(5)
+    X, R = rows(rng, N, M, dtype) + 0.5, rows(rng, N, M, dtype)
+    X = wl.round_to_bf16(X.astype(np.float32)) if dtype == "bf16" else X.astype(np.float32)
+    w = (1 + 0.1 * rng.standard_normal(M)).astype(np.float32)
+    Wg, Wu = (rows(rng, S, M, dtype, M ** -0.5) for _ in range(2))
+    dH, dStream = rows(rng, N, S, dtype, 0.1), rows(rng, N, M, dtype, 0.1)
+    e = lambda *s, k=t: torch.empty(*s, dtype=k, device=DEV)  # noqa: E731
+    d = b.conv_desc(N, M)
+    wsf, wsg = (workspace(b.fw_workspace_bytes(op, M, S, d, dt)) for op in (b.FW_OP_GATED_FORWARD, b.FW_OP_GATED_GRAD))
+    wsn = workspace(b.fw_workspace_bytes(b.FW_OP_RMS_NORM_GRAD, M, 0, d, dt))
+    wsc = workspace(b.fw_workspace_bytes(b.FW_OP_COV_ACCUMULATE, M, 0, d, dt))
+    wsd, wst = workspace(b.fw_workspace_bytes(b.FW_OP_COND_REDUCE_STEP, M)), workspace(b.fw_workspace_bytes(b.FW_OP_GRAD_TRANSFORM, M, S, None, dt))
+    Xd, Rd, wd, Wgd, Wud, dHd, dSd = dev(X, t), dev(R, t), dev(w), dev(Wg, t), dev(Wu, t), dev(dH, t), dev(dStream, t)
+    H, Y, A, Z, dY, dX, dw = e(N, M), e(N, M), e(N, S), e(2, N, S), e(N, M), e(N, M), e(M, k=torch.float32)
+    dWg, dWu, Gg, Gu = e(S, M), e(S, M), e(S, M), e(S, M)
+    f = lambda *s: torch.zeros(*s, device=DEV)  # noqa: E731
+    C, s1, mu, Phi, phi, lbar = f(M, M), f(M), f(M), f(M, M), f(M), f(4)
+    T, Q, Qs, Py, Psi, xi2, info = f(M, M), f(M, M), f(M, M), f(M, M), f(M, M), f(M), torch.zeros(8, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    b.fw_rms_norm(Xd, Rd, dt, N, M, wd, EPS, H, Y, stream=stream)
+    b.fw_cov_accumulate(Y, dt, b.FW_LAYOUT_ROWS, d, C, s1, wsc, stream=stream)
+    b.fw_cov_finalize(C, s1, N, M, 0.0, 1, mu, Phi, phi, lbar, stream=stream)
+    st = b.cond_state(M, Phi, lbar, T, Q, Qs, Py, Psi, xi2)
+    b.fw_cond_state_init(st, stream=stream)
+    b.fw_cond_reduce_step(st, b.cond_params(), info, wsd, stream=stream)
+    b.fw_gated_forward(Y, dt, N, M, S, Wgd, Wud, None, None, b.FW_ACT_SILU, A, Z, wsf, stream=stream)
+    b.fw_gated_grad(Y, dt, N, M, S, Wgd, Wud, Z, dHd, mu, dY, dWg, dWu, None, None, wsg, stream=stream)
+    b.fw_rms_norm_grad(H, dt, N, M, wd, EPS, dY, dSd, dX, dw, wsn, stream=stream)
+    for G, out in ((dWg, Gg), (dWu, Gu)):
+        b.fw_grad_transform(G, dt, S, M, None, Qs, out, wst, stream=stream)
+    torch.cuda.synchronize()
+    host = lambda x: x.float().cpu().numpy().astype(np.float64)  # noqa: E731
+    got = {k: host(v) for k, v in dict(H=H, Y=Y, A=A, dY=dY, dX=dX, dw=dw, dWg=dWg, dWu=dWu, Gg=Gg, Gu=Gu, mu=mu, Qs=Qs).items()}
+    return got, dict(X=X, R=R, w=w, Wg=Wg, Wu=Wu, dH=dH, dStream=dStream)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_whitened_block_end_to_end(dtype):
+    got, i = whitened_step(dtype)
+    # every step of the chain rounds to the type once; a result has at most eight such roundings behind it, added up without signs
+    tol = 8 * HALF["bf16"] if dtype == "bf16" else 1e-5
+    h = lo.f64(i["X"]) + lo.f64(i["R"])
+    y = lo.rms_norm(h, i["w"], EPS)
+    mu = y.mean(0)
+    dY, dWg, dWu, _, _ = lo.gated_grad(y, i["Wg"], i["Wu"], "silu", i["dH"], mu=mu)
+    dX, dw = lo.rms_norm_grad(h, i["w"], EPS, dY, i["dStream"])
+    want = dict(H=h, Y=y, A=lo.gated(y, i["Wg"], i["Wu"], "silu"), dY=dY, dX=dX, dw=dw, dWg=dWg, dWu=dWu, mu=mu, Gg=dWg @ got["Qs"], Gu=dWu @ got["Qs"])
+    for k, v in want.items():
+        assert relF(got[k], v) < tol, k
+
+
+def test_a_whitened_block_on_another_stream():
+    side = torch.cuda.Stream()
+    a, c = whitened_step("bf16")[0], whitened_step("bf16", side)[0]
+    for k in a:
+        assert np.array_equal(a[k], c[k]), k
+
+
+def test_layers_captured_and_replayed():
+    """Every call recorded into one graph; each replay on new contents of the same buffers gives what the eager calls give."""
+    N, M, S, t, dt = 48, 200, 120, torch.bfloat16, b.FW_BF16
+    rng = np.random.default_rng(8)
+    d = b.conv_desc(N, M)
+    e = lambda *s, k=t: torch.zeros(*s, dtype=k, device=DEV)  # noqa: E731
+    X, R, dH = e(N, M), e(N, M), e(N, S)
+    Wg, Wu, w = dev(rows(rng, S, M, "bf16", 0.1), t), dev(rows(rng, S, M, "bf16", 0.1), t), dev(np.ones(M, np.float32))
+    Wq, sw = e(S, M, k=torch.int8), e(S, k=torch.float32)
+    b.fw_int8_rows(Wg, dt, S, M, Wq, sw)
+    ops = (b.FW_OP_GATED_FORWARD, b.FW_OP_GATED_GRAD, b.FW_OP_RMS_NORM_GRAD, b.FW_OP_INT8_PRODUCT)
+    ws = [workspace(b.fw_workspace_bytes(op, M, S, d, dt)) for op in ops]
+
+    def calls(o):
+        b.fw_rms_norm(X, R, dt, N, M, w, EPS, o["H"], o["Y"], o["q"], o["qs"])
+        b.fw_gated_forward(o["Y"], dt, N, M, S, Wg, Wu, None, None, b.FW_ACT_GELU, o["A"], o["Z"], ws[0])
+        b.fw_gated_grad(o["Y"], dt, N, M, S, Wg, Wu, o["Z"], dH, w, o["dY"], o["dWg"], o["dWu"], o["dbg"], o["dbu"], ws[1])
+        b.fw_rms_norm_grad(o["H"], dt, N, M, w, EPS, o["dY"], None, o["dX"], o["dw"], ws[2])
+        b.fw_int8_product(o["q"], o["qs"], N, M, S, Wq, sw, None, o["P"], dt, ws[3])
+
+    def outputs():
+        f = torch.float32
+        return dict(H=e(N, M), Y=e(N, M), q=e(N, M, k=torch.int8), qs=e(N, k=f), A=e(N, S), Z=e(2, N, S), dY=e(N, M), dWg=e(S, M), dWu=e(S, M), dbg=e(S),
+                    dbu=e(S), dX=e(N, M), dw=e(M, k=f), P=e(N, S))
+
+    eager, kept = outputs(), outputs()
+    calls(kept)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(kept)
+    for turn in range(3):
+        for x, n in ((X, M), (R, M), (dH, S)):
+            x.copy_(dev(rows(rng, N, n, "bf16"), t))
+        calls(eager)
+        torch.cuda.synchronize()
+        for x in kept.values():
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in eager:
+            assert torch.equal(eager[k], kept[k]), (turn, k)
