@@ -180,7 +180,8 @@ def _keep(st, case, new):
         st["H"] = new(N, S)
         st["ws"] = space(fw.FW_OP_GATED_FORWARD, M, S, d, dt)
         if kind == "train":
-            st["Z"], st["dX"], st["dWg"], st["dWu"] = new(2, N, S), new(N, M), new(S, M), new(S, M)
+            st["Z"] = new(2, N, S, dt=torch.float32)
+            st["dX"], st["dWg"], st["dWu"] = new(N, M), new(S, M), new(S, M)
             if case["bias"]:
                 st["dbg"], st["dbu"] = new(S), new(S)
             st["ws_grad"] = space(fw.FW_OP_GATED_GRAD, M, S, d, dt)
