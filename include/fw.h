@@ -358,7 +358,8 @@ fw_status fw_cond_probe(const float* Phi_y, int M, const float* b0, int k, float
 /* ------------------------------------------------------------------------------------------------------------
  * (5) Layers of a language model around the whitening: what makes a layer's input rows X [N, M] (one row per token, the rows that
  * fw_cov_accumulate takes as FW_LAYOUT_ROWS), its products, its weight gradients G [S, M], and its answers in 8 bits.  N, M and S
- * need not be multiples of anything.  Limits of all of them: M <= 32768, S <= 65536.  The workspaces are asked for with
+ * need not be multiples of anything.  Limits of all of them: N <= 2097152, M <= 32768,
+ * S <= 65536.  The workspaces are asked for with
  * d = {N, M, 1, 1, 1, 1, 1, 0, 0}, the geometry of N rows.
  *
  * Norm by the root mean square of a row, with the residual's addition:
@@ -398,8 +399,9 @@ fw_status fw_rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float
  *   Wg, Wu  in   [S, M] element type `dt`
  *   bg, bu  in   [S] float32, each may be NULL
  *   H       out  [N, S] element type `dt`
- *   Z       out  [2, N, S] element type `dt`, or NULL: what the backward pass needs of g and u, Z[0] = u act'(g) and Z[1] = act(g).
- *                (These factors rather than g and u: one rounding to `dt` instead of the two of g and u reaches each gradient.)
+ *   Z       out  [2, N, S] float32, or NULL: what the backward pass needs of g and u, Z[0] = u act'(g) and Z[1] = act(g).
+ *                (The factors rather than g and u, and float32 for both types: a bfloat16 gradient then has two roundings behind it, of
+ *                dg or du and its own, 1.4 times the error of its own alone; with g and u in bfloat16 it would be twice that error.)
  *   ws      scratch, fw_workspace_bytes(FW_OP_GATED_FORWARD, M, S, d, dt) bytes
  * Products and sums: FW_BF16 bfloat16 products summed in float32, FW_F32 float32 accuracy.  g, u, the activation and H before its
  * rounding are float32.
@@ -411,14 +413,14 @@ typedef enum {
     FW_ACT_RELU = 3        /* max(g, 0), slope 0 at 0 */
 } fw_act;
 fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* bg,
-                           const float* bu, fw_act act, void* H, void* Z, void* ws, size_t ws_bytes, void* stream);
+                           const float* bu, fw_act act, void* H, float* Z, void* ws, size_t ws_bytes, void* stream);
 
 /* Its gradient:  dg = dH Z[0],  du = dH Z[1],
  *   dX = dg Wg + du Wu,    dWg = dg^T (X - 1 mu^T),  dWu = du^T (X - 1 mu^T),    dbg = sum_n dg,  dbu = sum_n du
  * With mu the mean that the layer's whitening subtracts, dWg and dWu are the gradients G of Sec. 3.1 that fw_grad_transform and
  * fw_sgd_update take (both projections have the same rows, hence the same Q).
  *   X, Wg, Wu   in   as in the forward pass
- *   Z           in   [2, N, S] element type `dt`, from the forward pass
+ *   Z           in   [2, N, S] float32, from the forward pass
  *   dH          in   [N, S] element type `dt`
  *   mu          in   [M] float32, or NULL for zero
  *   dX          out  [N, M] element type `dt`, or NULL
@@ -427,7 +429,7 @@ fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, cons
  *   ws          scratch, fw_workspace_bytes(FW_OP_GATED_GRAD, M, S, d, dt) bytes
  * FW_BF16: dg and du are rounded to bfloat16 for the products, the sums are float32 and each result is rounded once.
  */
-fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const void* Z,
+fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* Z,
                         const void* dH, const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws,
                         size_t ws_bytes, void* stream);
 

@@ -61,7 +61,7 @@ fw_status split_rows_apply(const float* rows, int n, int M, const float* Q, cons
 // sizes that the layers of language models take
 fw_status rows_check(fw_dtype dt, int N, int M, int S) {
     if (N <= 0 || M <= 0 || S <= 0 || !dtype_ok(dt)) return FW_ERR_INVALID_ARG;
-    return M > 32768 || S > 65536 ? FW_ERR_UNSUPPORTED : FW_OK;
+    return N > (1 << 21) || M > 32768 || S > 65536 ? FW_ERR_UNSUPPORTED : FW_OK;
 }
 template <class... P>
 bool all_aligned16(const P*... p) { return (aligned16(p) && ...); }
@@ -332,8 +332,8 @@ fw_status fw_rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float
 }
 
 fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu,
-                           fw_act act, void* H, void* Z, void* ws, size_t ws_bytes, void* stream) {
-    if (!X || !Wg || !Wu || !H || (int)act < FW_ACT_SILU || (int)act > FW_ACT_RELU || H == X || H == Z || (Z && Z == X)) return FW_ERR_INVALID_ARG;
+                           fw_act act, void* H, float* Z, void* ws, size_t ws_bytes, void* stream) {
+    if (!X || !Wg || !Wu || !H || (int)act < FW_ACT_SILU || (int)act > FW_ACT_RELU || H == X || H == (void*)Z || (Z && (const void*)Z == X)) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, S);
     if (rc != FW_OK) return rc;
     if (!all_aligned16(X, Wg, Wu, bg, bu, H, Z, ws)) return FW_ERR_ALIGNMENT;
@@ -342,10 +342,10 @@ fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, cons
     return gated_forward(X, dt, N, M, S, Wg, Wu, bg, bu, act, H, Z, ws, reinterpret_cast<hipStream_t>(stream));
 }
 
-fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const void* Z, const void* dH,
+fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* Z, const void* dH,
                         const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws, size_t ws_bytes, void* stream) {
     if (!X || !Wg || !Wu || !Z || !dH || !dWg != !dWu || !dbg != !dbu || (!dX && !dWg && !dbg)) return FW_ERR_INVALID_ARG;
-    if (dX && (dX == X || dX == dH || dX == Z)) return FW_ERR_INVALID_ARG;
+    if (dX && (dX == X || dX == dH || dX == (const void*)Z)) return FW_ERR_INVALID_ARG;
     if (dWg && (dWg == dWu || dWg == Wg || dWg == Wu || dWu == Wg || dWu == Wu)) return FW_ERR_INVALID_ARG;
     if (dbg && dbg == dbu) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, S);

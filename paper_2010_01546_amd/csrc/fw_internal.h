@@ -199,8 +199,8 @@ fw_status int8_rows(const void* X, fw_dtype dt, int N, int M, signed char* q, fl
 size_t gated_forward_workspace_bytes(fw_dtype dt, int N, int M, int S);
 size_t gated_grad_workspace_bytes(fw_dtype dt, int N, int M, int S);
 fw_status gated_forward(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu,
-                        fw_act act, void* H, void* Z, void* ws, hipStream_t st);
-fw_status gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const void* Z, const void* dH,
+                        fw_act act, void* H, float* Z, void* ws, hipStream_t st);
+fw_status gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* Z, const void* dH,
                      const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws, hipStream_t st);
 
 // ---- int8.hip

@@ -1,23 +1,92 @@
 // Product of rows in 8 bits with weights in 8 bits, a scale per token and per channel:
-//   Y[n][s] = sx[n] sw[s] sum_m Xq[n][m] Wq[s][m] + b[s],   the sums exact in 32-bit integers
+//   Y[n][s] = sx[n] sw[s] sum_m Xq[n][m] Wq[s][m] + b[s],   the sums exact in 32-bit integers (tile_product.h)
 #include "fw_internal.h"
 #include "tile_product.h"
 
 namespace fw {
+namespace {
 
-size_t int8_product_workspace_bytes(int, int, int) { return 0; }
+inline int up16(int m) { return (m + 15) / 16 * 16; }
 
-template <class T>
-static fw_status run(const signed char* Xq, const float* sx, int N, int M, int S, const signed char* Wq, const float* sw, const float* b, T* Y,
-                     hipStream_t st) {
-    return strided_product<int>(Xq, M, 1, Wq, M, 1, N, S, M, [=] __device__(long long r, int c, int v) {
-        Y[r * S + c] = (T)((float)v * sx[r] * sw[c] + (b ? b[c] : 0.f));
-    }, st);
+template <class T> struct ScaleEpilogue {
+    T* Y;
+    const float *sx, *sw, *b;
+    int N, S;
+    template <int NCT, class Acc> __device__ __forceinline__ void apply(int row0, int col0, const Acc (&acc)[NCT]) const {
+#pragma unroll
+        for (int t = 0; t < NCT; ++t) {
+            const int s = col0 + 32 * t;
+            if (s >= S) continue;
+            const float w = sw[s], c = b ? b[s] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int n = tile_row(row0, i);
+                if (n < N) Y[(size_t)n * S + s] = (T)((float)acc[t][i] * sx[n] * w + c);
+            }
+        }
+    }
+};
+
+// rows of M bytes to rows of Mp (a multiple of 16), zeros behind
+__global__ __launch_bounds__(256) void pad_bytes_kernel(const signed char* __restrict__ in, int M, int Mp, size_t n16, uint4* __restrict__ out) {
+    const int c16 = Mp / 16;
+    for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < n16; e += (size_t)gridDim.x * 256) {
+        const size_t r = e / c16;
+        const int m = 16 * (int)(e - r * c16);
+        const signed char* p = in + r * M + m;
+        union { uint4 v; signed char c[16]; } u;
+        if (m + 16 <= M) {
+            __builtin_memcpy(&u, p, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) u.c[i] = m + i < M ? p[i] : (signed char)0;
+        }
+        out[e] = u.v;
+    }
+}
+
+fw_status pad_bytes(const signed char* in, int R, int M, void* out, hipStream_t st) {
+    const size_t n = (size_t)R * (up16(M) / 16), blocks = (n + 255) / 256;
+    hipLaunchKernelGGL(pad_bytes_kernel, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, st, in, M, up16(M), n,
+                       reinterpret_cast<uint4*>(out));
+    FW_LAUNCH_CHECK();
+    return FW_OK;
+}
+
+TileProduct plan(int N, int M, int S) {
+    TileProduct g = {};
+    g.R = N; g.C = S; g.chunks = up16(M) / 16;
+    g.stages = g.part = (g.chunks + 3) / 4;
+    tile_plan(g, false);
+    return g;
+}
+size_t padded_bytes(int R, int M) { return M % 16 ? align_up((size_t)R * up16(M), 256) : 0; }
+
+}  // namespace
+
+size_t int8_product_workspace_bytes(int N, int M, int S) {
+    return padded_bytes(N, M) + padded_bytes(S, M) + tile_partial_bytes(plan(N, M, S));
 }
 
 fw_status int8_product(const signed char* Xq, const float* sx, int N, int M, int S, const signed char* Wq, const float* sw, const float* b,
-                       void* Y, fw_dtype dt, void*, hipStream_t st) {
-    return dt == FW_BF16 ? run(Xq, sx, N, M, S, Wq, sw, b, (__bf16*)Y, st) : run(Xq, sx, N, M, S, Wq, sw, b, (float*)Y, st);
+                       void* Y, fw_dtype dt, void* ws, hipStream_t st) {
+    char* w = reinterpret_cast<char*>(ws);
+    TileProduct g = plan(N, M, S);
+    g.a = reinterpret_cast<const char*>(Xq);
+    g.b0 = reinterpret_cast<const char*>(Wq);
+    if (M % 16) {            // 16-byte loads need aligned rows
+        fw_status rc = pad_bytes(Xq, N, M, w, st);
+        if (rc == FW_OK) rc = pad_bytes(Wq, S, M, w + padded_bytes(N, M), st);
+        if (rc != FW_OK) return rc;
+        g.a = w;
+        g.b0 = w + padded_bytes(N, M);
+    }
+    g.b1 = g.b0;
+    g.apitch = g.bpitch = up16(M);
+    g.partial = w ? w + padded_bytes(N, M) + padded_bytes(S, M) : nullptr;
+    if (dt == FW_BF16)
+        return tile_product<true, false, false, false>(g, ScaleEpilogue<__bf16>{reinterpret_cast<__bf16*>(Y), sx, sw, b, N, S}, st);
+    return tile_product<true, false, false, false>(g, ScaleEpilogue<float>{reinterpret_cast<float*>(Y), sx, sw, b, N, S}, st);
 }
 
 }  // namespace fw

@@ -194,7 +194,7 @@ def gated_inputs(N, M, S, dtype, bias):
 
 def run_forward(X, Wg, Wu, bg, bu, kind, dtype, keep=True):
     (N, M), S, t = X.shape, Wg.shape[0], TDT[dtype]
-    H, Z = Out(N, S, dtype=t), Out(2, N, S, dtype=t) if keep else None
+    H, Z = Out(N, S, dtype=t), Out(2, N, S, dtype=torch.float32) if keep else None
     ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_FORWARD, M, S, b.conv_desc(N, M), FDT[dtype]))
     ws.fill_(255)
     b.fw_gated_forward(dev(X, t), FDT[dtype], N, M, S, dev(Wg, t), dev(Wu, t), None if bg is None else dev(bg), None if bu is None else dev(bu),
@@ -217,8 +217,8 @@ def check_forward(H, Z, X, Wg, Wu, bg, bu, kind, dtype):
     # |act''| <= 1.2; the slope of relu is that of a g on the same side of zero
     sure = np.abs(g) > eg if kind == "relu" else np.ones_like(g, dtype=bool)
     tol = np.abs(u) * 1.2 * eg + 1.2 * eu + 16 * U32 * (1 + np.abs(g)) * np.abs(u)
-    within(np.where(sure, Z[0], 0), np.where(sure, u * da, 0), tol + np.abs(u * da) * HALF[dtype] + 1e-38, "Z[0]")
-    within(Z[1], a, 1.2 * eg + 16 * U32 * np.abs(g) + np.abs(a) * HALF[dtype] + 1e-38, "Z[1]")
+    within(np.where(sure, Z[0], 0), np.where(sure, u * da, 0), tol + 1e-38, "Z[0]")
+    within(Z[1], a, 1.2 * eg + 16 * U32 * np.abs(g) + 1e-38, "Z[1]")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -243,7 +243,7 @@ def test_gated_activations(N, kind, dtype):
 
 
 def rounded_product(a, c, dtype):
-    """dH times a factor as the block's gradient has it: exact in float32 for bfloat16 factors, rounded once to the type."""
+    """dH times a factor as the block's gradient has it: in float32, then rounded to the type."""
     p = (lo.f64(a) * c).astype(np.float32)
     return lo.f64(wl.round_to_bf16(p) if dtype == "bf16" else p)
 
@@ -273,12 +273,11 @@ def test_gated_gradient(N, M, S, dtype):
     within(dWu.host(), want[2], ((2 * N + 8) * U32 + more) * (au.T @ aX) + half * np.abs(want[2]), "dWu")
     within(dbg.host(), want[3], ((N + 4) * U32 + more) * ag.sum(0) + half * np.abs(want[3]), "dbg")
     within(dbu.host(), want[4], ((N + 4) * U32 + more) * au.sum(0) + half * np.abs(want[4]), "dbu")
-    # against the whole formula in 64 bits: the factors, dg and du, and the results have a rounding each, independent of each other
-    # (random-sign model: 3 of at most `half`); float32 adds its sums
+    # against the whole formula in 64 bits: dg and du and the results have a rounding each, of at most `half`; float32 adds its sums
     full = lo.gated_grad(X, Wg, Wu, kind, dH, bg, bu, mu)
     if kind != "relu":
         for got, w, what in zip((dX, dWg, dWu), full, ("dX", "dWg", "dWu")):
-            assert relF(got.host(), w) < (3 * half if dtype == "bf16" else 2e-5), what
+            assert relF(got.host(), w) < (2 * half + 1e-4 if dtype == "bf16" else 2e-5), what
     # one group of outputs at a time
     alone = [Out(N, M, dtype=t), Out(S, M, dtype=t), Out(S, M, dtype=t), Out(S, dtype=t), Out(S, dtype=t)]
     b.fw_gated_grad(Xd, dt, N, M, S, Wgd, Wud, Z.t, dHd, None, alone[0].t, None, None, None, None, ws)
@@ -336,7 +335,7 @@ def whitened_step(dtype, stream=None):
     wsc = workspace(b.fw_workspace_bytes(b.FW_OP_COV_ACCUMULATE, M, 0, d, dt))
     wsd, wst = workspace(b.fw_workspace_bytes(b.FW_OP_COND_REDUCE_STEP, M)), workspace(b.fw_workspace_bytes(b.FW_OP_GRAD_TRANSFORM, M, S, None, dt))
     Xd, Rd, wd, Wgd, Wud, dHd, dSd = dev(X, t), dev(R, t), dev(w), dev(Wg, t), dev(Wu, t), dev(dH, t), dev(dStream, t)
-    H, Y, A, Z, dY, dX, dw = e(N, M), e(N, M), e(N, S), e(2, N, S), e(N, M), e(N, M), e(M, k=torch.float32)
+    H, Y, A, Z, dY, dX, dw = e(N, M), e(N, M), e(N, S), e(2, N, S, k=torch.float32), e(N, M), e(N, M), e(M, k=torch.float32)
     dWg, dWu, Gg, Gu = e(S, M), e(S, M), e(S, M), e(S, M)
     f = lambda *s: torch.zeros(*s, device=DEV)  # noqa: E731
     C, s1, mu, Phi, phi, lbar = f(M, M), f(M), f(M), f(M, M), f(M), f(4)
@@ -403,7 +402,7 @@ def test_layers_captured_and_replayed():
 
     def outputs():
         f = torch.float32
-        return dict(H=e(N, M), Y=e(N, M), q=e(N, M, k=torch.int8), qs=e(N, k=f), A=e(N, S), Z=e(2, N, S), dY=e(N, M), dWg=e(S, M), dWu=e(S, M), dbg=e(S),
+        return dict(H=e(N, M), Y=e(N, M), q=e(N, M, k=torch.int8), qs=e(N, k=f), A=e(N, S), Z=e(2, N, S, k=f), dY=e(N, M), dWg=e(S, M), dWu=e(S, M), dbg=e(S),
                     dbu=e(S), dX=e(N, M), dw=e(M, k=f), P=e(N, S))
 
     eager, kept = outputs(), outputs()
