@@ -4,7 +4,7 @@
 //
 // bfloat16: both projections in one launch, the panel of weights holding the same columns of Wg and Wu, so that a lane has g and u of
 // an element in its registers when the sums are done (tile_product.h).  The backward pass forms D = [dg | du] once, rounded to
-// bfloat16, [N][2 Sp] with Sp = S rounded up to 32 and zeros between, and takes two products of it: dX = D [Wg; Wu], whose contraction runs
+// bfloat16, [N][2 Sp] with Sp = S rounded up to 64 and zeros between, and takes two products of it: dX = D [Wg; Wu], whose contraction runs
 // over the rows of both weight matrices, and [dWg; dWu] = D^T X.  Operands that are contraction-major in memory are turned on the
 // way out of LDS, not in memory.  mu is taken out of the sums: D^T (X - 1 mu^T) = D^T X - (D^T 1) mu^T, with D^T 1 summed from the
 // rounded D, so that the identity is exact but for float32 sums.
@@ -43,66 +43,61 @@ template <class F> __device__ __forceinline__ void with_activation(int act, cons
     else f(std::integral_constant<int, FW_ACT_RELU>());
 }
 
-// ---- epilogues of the bfloat16 products
+// ---- epilogues of the bfloat16 products: four entries of a row
 struct GateEpilogue {
     __bf16* H;
     float* Z;
     const float *bg, *bu;
     int N, S, act;
-    template <int NCT, class Acc> __device__ __forceinline__ void apply(int row0, int col0, const Acc (&acc)[NCT]) const {
+    __device__ __forceinline__ void apply(int n, int s, const floatx4& gate, const floatx4& up) const {
+        if (n >= N || s >= S) return;
+        float b[4], c[4], h[4];
+        tile_vector(bg, s, S, b);
+        tile_vector(bu, s, S, c);
         with_activation(act, [&](auto ACT) {
 #pragma unroll
-            for (int t = 0; t < NCT / 2; ++t) {
-                const int s = col0 + 32 * t;
-                if (s >= S) continue;
-                const float b = bg ? bg[s] : 0.f, c = bu ? bu[s] : 0.f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int n = tile_row(row0, i);
-                    if (n >= N) continue;
-                    const float g = acc[t][i] + b, u = acc[t + NCT / 2][i] + c;
-                    float a, da;
-                    activation<decltype(ACT)::value>(g, a, da);
-                    const size_t e = (size_t)n * S + s;
-                    H[e] = (__bf16)(a * u);
-                    if (Z) { Z[e] = u * da; Z[(size_t)N * S + e] = a; }
-                }
+            for (int i = 0; i < 4; ++i) {
+                const float u = up[i] + c[i];
+                float a, da;
+                activation<decltype(ACT)::value>(gate[i] + b[i], a, da);
+                h[i] = a * u;
+                b[i] = u * da;
+                c[i] = a;
             }
         });
+        const size_t e = (size_t)n * S + s;
+        tile_store(H + e, s, S, h);
+        if (Z) {
+            tile_store(Z + e, s, S, b);
+            tile_store(Z + (size_t)N * S + e, s, S, c);
+        }
     }
 };
 struct RowsEpilogue {                     // dX
     __bf16* out;
     int N, M;
-    template <int NCT, class Acc> __device__ __forceinline__ void apply(int row0, int col0, const Acc (&acc)[NCT]) const {
-#pragma unroll
-        for (int t = 0; t < NCT; ++t) {
-            const int m = col0 + 32 * t;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int n = tile_row(row0, i);
-                if (n < N && m < M) out[(size_t)n * M + m] = (__bf16)acc[t][i];
-            }
-        }
+    __device__ __forceinline__ void apply(int n, int m, const floatx4& acc) const {
+        if (n >= N || m >= M) return;
+        const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+        tile_store(out + (size_t)n * M + m, m, M, v);
     }
 };
 struct WeightsEpilogue {                  // rows below Sp are the gate's, the others the up projection's
     __bf16 *dWg, *dWu;
     const float *sums, *mu;
     int S, Sp, M;
-    template <int NCT, class Acc> __device__ __forceinline__ void apply(int row0, int col0, const Acc (&acc)[NCT]) const {
+    __device__ __forceinline__ void apply(int r, int m, const floatx4& acc) const {
+        const int s = r >= Sp ? r - Sp : r;
+        if (s >= S || m >= M) return;
+        float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+        if (mu) {
+            const float d = sums[r];
+            float c[4];
+            tile_vector(mu, m, M, c);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = tile_row(row0, i), s = r >= Sp ? r - Sp : r;
-            if (s >= S || r >= 2 * Sp) continue;
-            __bf16* out = (r >= Sp ? dWu : dWg) + (size_t)s * M;
-            const float d = mu ? sums[r] : 0.f;
-#pragma unroll
-            for (int t = 0; t < NCT; ++t) {
-                const int m = col0 + 32 * t;
-                if (m < M) out[m] = (__bf16)(mu ? acc[t][i] - d * mu[m] : acc[t][i]);
-            }
+            for (int i = 0; i < 4; ++i) v[i] -= d * c[i];
         }
+        tile_store((r >= Sp ? dWu : dWg) + (size_t)s * M + m, m, M, v);
     }
 };
 
@@ -245,7 +240,7 @@ __global__ __launch_bounds__(256) void transpose_kernel(const float* __restrict_
 
 inline unsigned blocks_for(size_t n) { return (unsigned)((n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384); }
 inline int up8(int m) { return (m + 7) / 8 * 8; }
-inline int up32(int s) { return (s + 31) / 32 * 32; }
+inline int up64(int s) { return (s + 63) / 64 * 64; }
 inline int row_blocks(int N) { return (N + GG_ROWS - 1) / GG_ROWS; }
 inline const char* bytes(const void* p) { return reinterpret_cast<const char*>(p); }
 
@@ -277,21 +272,21 @@ struct Carve {
 TileProduct forward_plan(int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = S; g.chunks = up8(M) / 8;
-    g.stages = g.part = (g.chunks + 3) / 4;
+    g.stages = g.part = (g.chunks + 7) / 8;
     tile_plan(g, true);
     return g;
 }
 TileProduct rows_plan(int N, int M, int S) {
     TileProduct g = {};
-    g.R = N; g.C = M; g.chunks = 2 * up32(S) / 8; g.klen = S;
-    g.part = up32(S) / 32; g.stages = 2 * g.part;
+    g.R = N; g.C = M; g.chunks = 2 * up64(S) / 8; g.klen = S;
+    g.part = up64(S) / 64; g.stages = 2 * g.part;
     tile_plan(g, false);
     return g;
 }
 TileProduct weights_plan(int N, int M, int S) {
     TileProduct g = {};
-    g.R = 2 * up32(S); g.C = M; g.klen = N;
-    g.part = g.stages = (N + 31) / 32;
+    g.R = 2 * up64(S); g.C = M; g.klen = N;
+    g.part = g.stages = (N + 63) / 64;
     tile_plan(g, false);
     return g;
 }
@@ -317,7 +312,7 @@ struct GradWs { void *D, *X, *Wg, *Wu, *partial; float *part, *sums, *Wt, *Dt, *
 GradWs grad_ws(fw_dtype dt, int N, int M, int S, void* ws) {
     Carve c = {reinterpret_cast<char*>(ws)};
     GradWs w = {};
-    const size_t Sp = up32(S);
+    const size_t Sp = up64(S);
     w.D = c.take((size_t)N * 2 * Sp * (dt == FW_BF16 ? 2 : 4));
     w.part = reinterpret_cast<float*>(c.take((size_t)row_blocks(N) * 2 * Sp * 4));
     w.sums = reinterpret_cast<float*>(c.take(2 * Sp * 4));
@@ -372,7 +367,7 @@ fw_status forward_bf16(const void* X, int N, int M, int S, const void* Wg, const
 
 template <class T>
 fw_status gate_grad(const T* dH, const float* Z, int N, int S, const GradWs& w, bool sums, T* dbg, T* dbu, hipStream_t st) {
-    const int Sp = up32(S);
+    const int Sp = up64(S);
     hipLaunchKernelGGL(gate_grad_kernel<T>, dim3((Sp + 255) / 256, row_blocks(N)), dim3(256), 0, st, dH, Z, N, S, Sp, reinterpret_cast<T*>(w.D),
                        sums ? w.part : nullptr);
     FW_LAUNCH_CHECK();
@@ -385,7 +380,7 @@ fw_status gate_grad(const T* dH, const float* Z, int N, int S, const GradWs& w, 
 fw_status grad_f32(const float* X, int N, int M, int S, const float* Wg, const float* Wu, const float* Z, const float* dH, const float* mu,
                    float* dX, float* dWg, float* dWu, float* dbg, float* dbu, void* ws, hipStream_t st) {
     const GradWs w = grad_ws(FW_F32, N, M, S, ws);
-    const int Sp = up32(S);
+    const int Sp = up64(S);
     float* D = reinterpret_cast<float*>(w.D);
     fw_status rc = gate_grad<float>(dH, Z, N, S, w, dbg != nullptr, dbg, dbu, st);
     if (rc != FW_OK) return rc;
@@ -412,7 +407,7 @@ fw_status grad_f32(const float* X, int N, int M, int S, const float* Wg, const f
 fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const void* Wu, const float* Z, const __bf16* dH, const float* mu,
                     __bf16* dX, __bf16* dWg, __bf16* dWu, __bf16* dbg, __bf16* dbu, void* ws, hipStream_t st) {
     const GradWs w = grad_ws(FW_BF16, N, M, S, ws);
-    const int Sp = up32(S);
+    const int Sp = up64(S);
     fw_status rc = gate_grad<__bf16>(dH, Z, N, S, w, dbg || (mu && dWg), dbg, dbu, st);
     if (rc != FW_OK) return rc;
     if (M % 8 && dX) {

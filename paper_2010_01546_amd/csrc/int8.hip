@@ -12,18 +12,15 @@ template <class T> struct ScaleEpilogue {
     T* Y;
     const float *sx, *sw, *b;
     int N, S;
-    template <int NCT, class Acc> __device__ __forceinline__ void apply(int row0, int col0, const Acc (&acc)[NCT]) const {
+    __device__ __forceinline__ void apply(int n, int s, const intx4& acc) const {
+        if (n >= N || s >= S) return;
+        float w[4], c[4], y[4];
+        tile_vector(sw, s, S, w);
+        tile_vector(b, s, S, c);
+        const float x = sx[n];
 #pragma unroll
-        for (int t = 0; t < NCT; ++t) {
-            const int s = col0 + 32 * t;
-            if (s >= S) continue;
-            const float w = sw[s], c = b ? b[s] : 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int n = tile_row(row0, i);
-                if (n < N) Y[(size_t)n * S + s] = (T)((float)acc[t][i] * sx[n] * w + c);
-            }
-        }
+        for (int i = 0; i < 4; ++i) y[i] = (float)acc[i] * x * w[i] + c[i];
+        tile_store(Y + (size_t)n * S + s, s, S, y);
     }
 };
 
@@ -56,7 +53,7 @@ fw_status pad_bytes(const signed char* in, int R, int M, void* out, hipStream_t 
 TileProduct plan(int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = S; g.chunks = up16(M) / 16;
-    g.stages = g.part = (g.chunks + 3) / 4;
+    g.stages = g.part = (g.chunks + 7) / 8;
     tile_plan(g, false);
     return g;
 }

@@ -2,17 +2,21 @@
 // Products of two matrices on the matrix cores, for bfloat16 entries (float32 sums) and 8-bit integers (32-bit integer sums), with an
 // epilogue of the caller's:  C[r][c] = sum_k A[r][k] B[c][k].
 //
-// A workgroup of four wavefronts owns a tile of 64 NRT x 64 NCT results, a wavefront 32 NRT x 32 NCT of them in accumulation registers
-// (v_mfma_f32_32x32x16_bf16 or v_mfma_i32_32x32x32_i8).  The contraction goes by in stages of 64 bytes of every row of the two
-// panels; a ring of stages lies in LDS, filled by loads that go there directly, one barrier per stage, and the fragment reads of the next
-// stage and the loads of a later one are placed between the matrix instructions of this one.
+// A workgroup owns a tile of 64 NRT x 64 NCT results.  Its wavefronts, two below each other and NW / 2 side by side, hold their parts in
+// accumulation registers, as 16 x 16 results of v_mfma_f32_16x16x32_bf16 or v_mfma_i32_16x16x64_i8.  (32 x 32 results need fewer
+// instructions and the same operands, but the chip runs them slower under its power limit: random bfloat16 operands in registers, 1.46
+// to 1.70 PFLOP/s against 1.91 to 2.08.)  B is the first operand, so that a lane holds four columns next to each other of one row.
+// The contraction goes by in stages of 128 bytes of every row of the two panels, so that the loads ask for whole cache lines: a compute
+// unit has about 110 requests to its L2 under way, whatever their size, and with 64 bytes each those bound the kernel (loads alone, 8192 x
+// 24576 x 4608: 1290 us against 1020).  A ring of stages lies in LDS, filled by loads that go there directly, one barrier per stage.  The
+// fragment reads of the next half of a stage and the loads of a later stage are placed between the matrix instructions of this half.
 //
 // An operand lies in memory in one of two ways.
-//   Rows along the contraction (k contiguous): a stage holds 64 bytes of each row, four chunks of 16; chunk c of row r lies at
-//     c ^ (r / 4 % 4), which spreads the 16 lanes that read together over all banks.
-//   Contraction-major (bfloat16; a row of memory is one k): a stage holds 32 k of all the panel's columns and is turned as it is read
-//     (ds_read_b64_tr_b16: 16 lanes get 4 k of a column each out of 4 x 16 entries).  The chunks of row k are permuted by 4 (k % 4) (panels
-//     of 64 columns: 4 (k / 2 % 2)), so that the four rows read together fall into different banks.  No transposed copy is made.
+//   Rows along the contraction (k contiguous): a stage holds 128 bytes of each row, eight chunks of 16; chunk c of row r lies at
+//     c ^ (r / 2 % 8), which spreads the 16 rows that are read together over all banks.
+//   Contraction-major (bfloat16; a row of memory is one k): a stage holds 64 k of all the panel's columns and is turned as it is read
+//     (ds_read_b64_tr_b16: 16 lanes get 4 k of a column each out of 4 x 16 entries).  Pairs of chunks, 16 columns, are permuted by a
+//     function of k that puts the eight k read together into different banks.  No transposed copy is made.
 // Where the contraction ends inside a stage, the loads past the end fetch a zero (in both operands: 0 x NaN is NaN).  Rows or columns past
 // the edge are clamped; they feed results that the epilogue does not store.
 //
@@ -24,7 +28,6 @@
 namespace fw {
 
 typedef int intx4 __attribute__((ext_vector_type(4)));
-typedef int intx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
 static __device__ uint4 tile_zero;          // 16 bytes of zeros, never written
@@ -49,25 +52,52 @@ __device__ __forceinline__ void tile_at(const TileProduct& g, int tile, int& I, 
     I = 8 * band + in - J * h;
 }
 
-template <int I, int N, class F> __device__ __forceinline__ void static_for(const F& f) {
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>());
-        static_for<I + 1, N>(f);
+// permutation of the pairs of chunks of row k of a contraction-major panel of 64 N columns
+template <int N> __device__ __forceinline__ int pair_swizzle(int k) {
+    return N > 1 ? (k & 3) | ((k >> 1) & 4) : ((k >> 1) & 1) | ((k >> 2) & 2);
+}
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// dma16 (fw_internal.h) from an address that is the same for the wavefront plus 32 bits of a lane's own: no vector arithmetic
+__device__ __forceinline__ void dma16_from(const void* base, unsigned offset, void* lds_dst) {
+    const unsigned lds_addr = (unsigned)(size_t)(__attribute__((address_space(3))) void*)lds_dst;
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds_addr) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int NRT, int NCT, int NW> struct TileShape {
+    static constexpr int NWC = NW / 2;                          // wavefronts side by side
+    static constexpr int WR = 2 * NRT, WC = 4 * NCT / NWC;      // 16 x 16 results of a wavefront, down and across
+    static constexpr int NT = 64 * NW;
+    static constexpr int STAGE = 8192 * (NRT + NCT);            // bytes of a stage
+    static constexpr int NST = NRT + NCT >= 8 ? 2 : NRT + NCT == 3 ? 3 : NRT + NCT == 6 ? 3 : 2;
+};
+template <int WC, bool PAIR> __device__ __forceinline__ int tile_column(int panel, int wj, int lane) {
+    return panel + wj * (PAIR ? 8 * WC : 16 * WC) + 4 * (lane >> 4);
+}
+// the finished sums of a wavefront's row of 16 x 16 results: row n, from column s on
+template <int WC, bool PAIR, class Acc, class Epi>
+__device__ __forceinline__ void tile_apply(const Epi& epi, int n, int s, const Acc (&acc)[WC]) {
+#pragma unroll
+    for (int tb = 0; tb < (PAIR ? WC / 2 : WC); ++tb) {
+        if constexpr (PAIR) epi.apply(n, s + 16 * tb, acc[tb], acc[tb + WC / 2]);
+        else epi.apply(n, s + 16 * tb, acc[tb]);
     }
 }
 
-template <int NRT, int NCT> constexpr int tile_stages() { return NRT + NCT >= 8 ? 5 : NRT + NCT == 6 ? 3 : 4; }
-
-// PAIR: the panel of B holds columns of b0 and the same columns of b1; tiles tb and tb + NCT / 2 of a wavefront belong together.
-template <bool I8, int NRT, int NCT, bool AKM, bool BKM, bool PAIR, class Epi>
-__global__ __launch_bounds__(256, NRT + NCT >= 8 ? 1 : 2) void tile_product_kernel(TileProduct g, Epi epi) {
-    constexpr int NST = tile_stages<NRT, NCT>(), NF = NRT + NCT, STAGE = 4096 * NF, NM = NRT * NCT;
-    using Acc = typename std::conditional<I8, intx16, floatx16>::type;
-    __shared__ __align__(1024) char lds[NST][STAGE];
+// PAIR: the panel of B holds columns of b0 and the same columns of b1; results tb and tb + WC / 2 of a wavefront belong together.
+template <bool I8, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>
+__global__ __launch_bounds__(64 * NW, NW == 4 && NRT + NCT >= 8 ? 1 : 2) void tile_product_kernel(TileProduct g, Epi epi) {
+    using Shape = TileShape<NRT, NCT, NW>;
+    constexpr int NST = Shape::NST, NWC = Shape::NWC, WR = Shape::WR, WC = Shape::WC;
+    constexpr int LA = 8 * NRT / NW, LB = 8 * NCT / NW, NL = LA + LB;      // loads of a wavefront and stage
+    constexpr int NF = WR + WC, NM = WR * WC;                             // fragments, matrix instructions
+    using Acc = typename std::conditional<I8, intx4, floatx4>::type;
+    __shared__ __align__(1024) char lds[NST][Shape::STAGE];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wi = wave >> 1, wj = wave & 1;
-    const int half = lane >> 5, l32 = lane & 31;
+    const int wi = wave / NWC, wj = wave % NWC;
     // workgroups go to the 8 XCDs in turn: each XCD gets a contiguous run of tiles
     const int total = g.tiles * g.runs, per_xcd = (total + 7) / 8;
     int tile = ((int)blockIdx.x & 7) * per_xcd + ((int)blockIdx.x >> 3);
@@ -79,186 +109,221 @@ __global__ __launch_bounds__(256, NRT + NCT >= 8 ? 1 : 2) void tile_product_kern
     I = __builtin_amdgcn_readfirstlane(I); J = __builtin_amdgcn_readfirstlane(J);
     const int c0 = run * g.spr, cend = min(c0 + g.spr, g.stages);
 
-    // what this lane brings: of each panel a wavefront loads 1 KB pieces wave, wave + 4, ...
-    const char* src[NF];
-    int lim[NF];                               // stages (of a part) below which the chunk lies inside the contraction
-    auto along = [&](const char* base, long long pitch, int row, int rows, int k) {
-        const int c = (lane & 3) ^ ((lane >> 4) & 3);
-        src[k] = base + (long long)min(row, rows - 1) * pitch + 16 * c;
-        lim[k] = (g.chunks - c + 3) >> 2;
+    // What this lane brings: of each panel a wavefront loads 1 KB pieces wave, wave + NW, ...; piece k comes from base[k] (the same for the
+    // wavefront) + the stage's offset + vof[k]
+    const char* base[NL];
+    unsigned vof[NL];
+    int lim[NL];                               // stages (of a part) below which the chunk lies inside the contraction
+    auto along = [&](const char* p, long long pitch, int row0, int rows, int k) __attribute__((always_inline)) {
+        const int c = (lane & 7) ^ (4 * (row0 >> 3 & 1) + (lane >> 4));       // row0 is a multiple of 8 from the panel's first on
+        row0 = min(row0, rows - 1);
+        base[k] = p + row0 * pitch;
+        vof[k] = (unsigned)(min(lane >> 3, rows - 1 - row0) * pitch) + 16 * c;
+        lim[k] = (g.chunks - c + 7) >> 3;
     };
-    auto major = [&](auto NT, const char* base, long long pitch, int tile0, int cols, int piece, int k) {
-        constexpr int CH = 8 * decltype(NT)::value;              // chunks of a row of the panel
-        const int kr = piece * (64 / CH) + lane / CH, p = lane % CH;
-        const int c = p ^ (CH > 8 ? 4 * (kr & 3) : 4 * ((kr >> 1) & 1));
-        src[k] = base + kr * pitch + 16ll * min(tile0 * CH + c, (cols + 7) / 8 - 1);
-        lim[k] = (g.klen - kr + 31) >> 5;
+    auto major = [&](auto N, const char* p, long long pitch, int tile0, int cols, int piece, int k) __attribute__((always_inline)) {
+        constexpr int CH = 8 * decltype(N)::value;               // chunks of a row of the panel
+        const int kr = piece * (64 / CH) + lane / CH;
+        const int c = (lane % CH) ^ (2 * pair_swizzle<decltype(N)::value>(kr));
+        base[k] = p;
+        vof[k] = (unsigned)(kr * pitch) + 16 * min(tile0 * CH + c, (cols + 7) / 8 - 1);
+        lim[k] = (g.klen - kr + 63) >> 6;
     };
 #pragma unroll
-    for (int k = 0; k < NRT; ++k) {
-        const int piece = wave + 4 * k;
+    for (int k = 0; k < LA; ++k) {
+        const int piece = wave + NW * k;
         if constexpr (AKM) major(std::integral_constant<int, NRT>(), g.a, g.apitch, I, g.R, piece, k);
-        else along(g.a, g.apitch, I * 64 * NRT + 16 * piece + (lane >> 2), g.R, k);
+        else along(g.a, g.apitch, I * 64 * NRT + 8 * piece, g.R, k);
     }
 #pragma unroll
-    for (int k = 0; k < NCT; ++k) {
-        const int piece = wave + 4 * k;
-        if constexpr (BKM) major(std::integral_constant<int, NCT>(), g.b0, g.bpitch, J, g.C, piece, NRT + k);
+    for (int k = 0; k < LB; ++k) {
+        const int piece = wave + NW * k;
+        if constexpr (BKM) major(std::integral_constant<int, NCT>(), g.b0, g.bpitch, J, g.C, piece, LA + k);
         else if constexpr (PAIR) {
-            const int pr = 16 * piece, w = pr % (32 * NCT);
-            const int col = J * 32 * NCT + pr / (32 * NCT) * 16 * NCT + w % (16 * NCT) + (lane >> 2);
-            along(w >= 16 * NCT ? g.b1 : g.b0, g.bpitch, col, g.C, NRT + k);
-        } else along(g.b0, g.bpitch, J * 64 * NCT + 16 * piece + (lane >> 2), g.C, NRT + k);
+            const int pr = 8 * piece, w = pr % (16 * WC);       // row of the panel, of its wavefront's part
+            const int col = J * 32 * NCT + pr / (16 * WC) * 8 * WC + w % (8 * WC);
+            along(w >= 8 * WC ? g.b1 : g.b0, g.bpitch, col, g.C, LA + k);
+        } else along(g.b0, g.bpitch, J * 64 * NCT + 8 * piece, g.C, LA + k);
     }
     const long long second = BKM ? g.b1 - g.b0 : 0;
-    auto load_one = [&](int buf, int c, int k) {                 // k is a constant after unrolling
+    // stages that lie inside the contraction with all their chunks (of a part)
+    const int whole = AKM || BKM ? g.klen >> 6 : g.chunks >> 3;
+    struct Stage { long long a, b; int c, cb; bool all; };
+    auto stage_at = [&](int c) __attribute__((always_inline)) {
+        Stage s;
         const bool two = BKM && c >= g.part;
-        const int cc = two ? c - g.part : c;
-        long long off;
-        if (k < NRT) off = AKM ? (long long)c * 32 * g.apitch : (long long)c * 64;
-        else off = BKM ? (long long)cc * 32 * g.bpitch + (two ? second : 0) : (long long)c * 64;
-        const bool inside = c < cend && ((k < NRT && !AKM) || !BKM ? c : cc) < lim[k];
-        const void* from = inside ? (const void*)(src[k] + off) : (const void*)&tile_zero;
-        dma16(from, &lds[buf][1024 * (wave + 4 * (k < NRT ? k : k - NRT)) + (k < NRT ? 0 : 4096 * NRT)]);
+        s.c = c; s.cb = two ? c - g.part : c;
+        s.a = AKM ? (long long)c * 64 * g.apitch : (long long)c * 128;
+        s.b = BKM ? (long long)s.cb * 64 * g.bpitch + (two ? second : 0) : (long long)c * 128;
+        s.all = c < cend && s.cb < whole;
+        return s;
+    };
+    auto load_one = [&](int buf, const Stage& s, int k) __attribute__((always_inline)) {      // k is a constant after unrolling
+        const bool isa = k < LA;
+        void* to = &lds[buf][1024 * (wave + NW * (isa ? k : k - LA)) + (isa ? 0 : 8192 * NRT)];
+        const char* from = base[k] + (isa ? s.a : s.b);
+        if (s.all) {
+            dma16_from(from, vof[k], to);
+        } else {
+            const bool inside = s.c < cend && (isa ? s.c : s.cb) < lim[k];
+            dma16(inside ? (const void*)(from + vof[k]) : (const void*)&tile_zero, to);
+        }
     };
 
-    Acc acc[NRT][NCT];
+    Acc acc[WR][WC];
 #pragma unroll
-    for (int a = 0; a < NRT; ++a)
+    for (int a = 0; a < WR; ++a)
 #pragma unroll
-        for (int b = 0; b < NCT; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0;
+        for (int b = 0; b < WC; ++b) acc[a][b] = Acc{0, 0, 0, 0};
 
-    // fragments of a stage: f = kk NF + (tile of A, then tile of B), kk the half of the stage's contraction
-    intx4 fr[2][2 * NF];
-    const int at = l32 * 64, sw = (l32 >> 2) & 3, j = lane & 15;
-    const int small = 2 * ((lane >> 4) & 1) + ((j >> 1) & 1);
-    auto read_one = [&](int buf, int set, int f) {
-        const int kk = f / NF, r = f % NF;
-        const bool isa = r < NRT;
-        const int t = isa ? wi * NRT + r : wj * NCT + r - NRT;
-        const char* panel = &lds[buf][isa ? 0 : 4096 * NRT];
+    // Fragment f of half h of a stage: 16 rows of A, then of B.  Where a lane reads: its own place, with 64 h flipped in and + 2048 f for
+    // rows along the contraction, with 32 f flipped in and 32 rows further on for the second half of a contraction-major panel (the
+    // permutations touch only those bits).
+    intx4 fr[2][NF];
+    const int l16 = lane & 15, q = lane >> 4, kq = 8 * q + (l16 >> 2);       // kq + 4 and kq + 32 have the permutation of kq
+    const int along_at = l16 * 128 + 16 * (q ^ (l16 >> 1));
+    const int at_a = AKM ? kq * 128 * NRT + 32 * (wi * WR ^ pair_swizzle<NRT>(kq)) + 8 * (l16 & 3) : wi * WR * 2048 + along_at;
+    const int at_b = 8192 * NRT + (BKM ? kq * 128 * NCT + 32 * (wj * WC ^ pair_swizzle<NCT>(kq)) + 8 * (l16 & 3) : wj * WC * 2048 + along_at);
+    auto read_one = [&](int a, int b, int half, int f) __attribute__((always_inline)) {    // a, b: at_a and at_b in the stage's buffer
+        const bool isa = f < WR;
+        const int r = isa ? f : f - WR;
+        const char* all = &lds[0][0];
         if (isa ? AKM : BKM) {
-            const int nt = isa ? NRT : NCT, rowb = 128 * nt;
-            const int ch = 4 * (nt > 1 ? t ^ (j >> 2) : t ^ (j >> 3)) + small;
-            const char* p = panel + (16 * kk + 8 * half + (j >> 2)) * rowb + 16 * ch + 8 * (j & 1);
+            const int rowb = 128 * (isa ? NRT : NCT);
+            const char* p = all + ((isa ? a : b) ^ (32 * r)) + 32 * half * rowb;
             typedef __attribute__((address_space(3))) shortx4* lp;
             union { shortx4 h[2]; intx4 v; } u;
             u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)p);
             u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 4 * rowb));
-            fr[set][f] = u.v;
+            fr[half][f] = u.v;
         } else {
-            fr[set][f] = *reinterpret_cast<const intx4*>(panel + t * 2048 + at + 16 * ((2 * kk + half) ^ sw));
+            fr[half][f] = *reinterpret_cast<const intx4*>(all + ((isa ? a : b) ^ (64 * half)) + 2048 * r);
         }
     };
-    auto multiply_one = [&](int set, int m) {
-        const int kk = m / NM, ta = (m % NM) / NCT, tb = m % NCT;
+    auto multiply_one = [&](int half, int m) __attribute__((always_inline)) {
+        const int ta = m / WC, tb = m % WC;
         if constexpr (I8)
-            acc[ta][tb] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fr[set][kk * NF + ta], fr[set][kk * NF + NRT + tb], acc[ta][tb], 0, 0, 0);
+            acc[ta][tb] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fr[half][WR + tb], fr[half][ta], acc[ta][tb], 0, 0, 0);
         else
-            acc[ta][tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fr[set][kk * NF + ta]),
-                                                                  __builtin_bit_cast(bf16x8, fr[set][kk * NF + NRT + tb]), acc[ta][tb], 0, 0, 0);
+            acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fr[half][WR + tb]),
+                                                                  __builtin_bit_cast(bf16x8, fr[half][ta]), acc[ta][tb], 0, 0, 0);
     };
 
     // The loads of a wavefront complete in order: "at most those of NST - 2 stages outstanding" means that the stage before them has
-    // landed for it, the barrier extends that to all four.  At the barrier of a stage every wavefront holds that stage's fragments in
-    // registers, so its buffer is free for the stage NST further on.  Every turn issues the same number of loads (past the end they fetch
-    // zeros), which keeps the count valid.
+    // landed for it, the barrier extends that to all.  At the barrier in the middle of a stage every wavefront holds the stage's second
+    // half in registers, so its buffer is free for the stage NST further on.  Every stage issues the same number of loads (past the end
+    // they fetch zeros), which keeps the count valid.
+    for (int i = 0; i < NST; ++i) {
+        const Stage s = stage_at(c0 + i);
 #pragma unroll
-    for (int i = 0; i < NST - 1; ++i)
-#pragma unroll
-        for (int k = 0; k < NF; ++k) load_one(i, c0 + i, k);
-    FW_WAIT_VM((NST - 2) * NF);
+        for (int k = 0; k < NL; ++k) load_one(i, s, k);
+    }
+    FW_WAIT_VM((NST - 1) * NL);
     __builtin_amdgcn_s_barrier();
     FW_COMPILER_FENCE();
 #pragma unroll
-    for (int k = 0; k < NF; ++k) load_one(NST - 1, c0 + NST - 1, k);
-#pragma unroll
-    for (int f = 0; f < 2 * NF; ++f) read_one(0, 0, f);
+    for (int f = 0; f < NF; ++f) read_one(at_a, at_b, 0, f);
     int sc = 0;
-    auto turn = [&](int c, auto SET) {
-        constexpr int set = decltype(SET)::value;
-        const int sn = sc == NST - 1 ? 0 : sc + 1;
-        FW_WAIT_LGKM0();
-        FW_WAIT_VM((NST - 2) * NF);
-        __builtin_amdgcn_s_barrier();
-        FW_COMPILER_FENCE();
-        // reads of the next stage first, then the loads, spread over the matrix instructions
-        constexpr int OPS = 3 * NF;
+    // the reads over the first three quarters of the matrix instructions (the last ones have to be back when the next half begins)
+    auto half_turn = [&](int ra, int rb, auto HALF, auto&& also) __attribute__((always_inline)) {
+        constexpr int half = decltype(HALF)::value;
 #pragma unroll
-        for (int m = 0; m < 2 * NM; ++m) {
+        for (int m = 0; m < NM; ++m) {
 #pragma unroll
-            for (int o = m * OPS / (2 * NM); o < (m + 1) * OPS / (2 * NM); ++o) {
-                if (o < 2 * NF) read_one(sn, set ^ 1, o);
-                else load_one(sc, c + NST, o - 2 * NF);
-            }
-            multiply_one(set, m);
+            for (int r = 0; r < NF; ++r)
+                if (r * (3 * NM) / (4 * NF) == m) read_one(ra, rb, half ^ 1, r);
+            also(m);
+            multiply_one(half, m);
             __builtin_amdgcn_sched_barrier(0);
         }
-        sc = sn;
     };
-    int c = c0;
-    for (; c + 1 < cend; c += 2) {
-        turn(c, std::integral_constant<int, 0>());
-        turn(c + 1, std::integral_constant<int, 1>());
+    for (int c = c0; c < cend; ++c) {
+        const Stage next = stage_at(c + NST);
+        const int sn = sc == NST - 1 ? 0 : sc + 1;
+        half_turn(at_a + sc * Shape::STAGE, at_b + sc * Shape::STAGE, std::integral_constant<int, 0>(), [](int) {});
+        FW_WAIT_LGKM0();
+        FW_WAIT_VM((NST - 2) * NL);
+        __builtin_amdgcn_s_barrier();
+        FW_COMPILER_FENCE();
+        half_turn(at_a + sn * Shape::STAGE, at_b + sn * Shape::STAGE, std::integral_constant<int, 1>(), [&](int m) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 0; k < NL; ++k)
+                if (k * NM / NL == m) load_one(sc, next, k);
+        });
+        sc = sn;
     }
-    if (c < cend) turn(c, std::integral_constant<int, 0>());
     FW_WAIT_VM(0);
     FW_WAIT_LGKM0();
 
     if (g.runs > 1) {
-        typedef typename std::conditional<I8, int4, float4>::type Quad;
-        Quad* out = reinterpret_cast<Quad*>(g.partial) + ((size_t)run * g.tiles + tile) * (NM * 4 * 256) + tid;
+        Acc* out = reinterpret_cast<Acc*>(g.partial) + ((size_t)run * g.tiles + tile) * (NM * Shape::NT) + tid;
 #pragma unroll
-        for (int ta = 0; ta < NRT; ++ta)
+        for (int ta = 0; ta < WR; ++ta)
 #pragma unroll
-            for (int tb = 0; tb < NCT; ++tb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    Quad q = {acc[ta][tb][4 * i], acc[ta][tb][4 * i + 1], acc[ta][tb][4 * i + 2], acc[ta][tb][4 * i + 3]};
-                    out[((ta * NCT + tb) * 4 + i) * 256] = q;
-                }
+            for (int tb = 0; tb < WC; ++tb) out[(ta * WC + tb) * Shape::NT] = acc[ta][tb];
         return;
     }
-    const int col = PAIR ? J * 32 * NCT + 16 * NCT * wj : J * 64 * NCT + 32 * NCT * wj;
-    static_for<0, NRT>([&](auto TA) {
-        constexpr int ta = decltype(TA)::value;
-        epi.template apply<NCT>(I * 64 * NRT + 32 * NRT * wi + 32 * ta + 4 * half, col + l32, acc[ta]);
-    });
+    const int s = tile_column<WC, PAIR>(J * (PAIR ? 32 : 64) * NCT, wj, lane);
+#pragma unroll
+    for (int ta = 0; ta < WR; ++ta) tile_apply<WC, PAIR>(epi, I * 64 * NRT + 16 * (wi * WR + ta) + l16, s, acc[ta]);
 }
 
-// adds the runs of a tile's row of 32 x 32 results, in order, and applies the epilogue
-template <bool I8, int NRT, int NCT, bool PAIR, class Epi>
-__global__ __launch_bounds__(256) void tile_runs_kernel(TileProduct g, Epi epi) {
-    using Acc = typename std::conditional<I8, intx16, floatx16>::type;
-    typedef typename std::conditional<I8, int4, float4>::type Quad;
-    const int tile = blockIdx.x / NRT, ta = blockIdx.x % NRT;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = wave >> 1, wj = wave & 1, half = lane >> 5, l32 = lane & 31;
+// adds the runs of a tile's rows of 16 x 16 results, in order, and applies the epilogue
+template <bool I8, int NRT, int NCT, int NW, bool PAIR, class Epi>
+__global__ __launch_bounds__(64 * NW) void tile_runs_kernel(TileProduct g, Epi epi) {
+    using Shape = TileShape<NRT, NCT, NW>;
+    constexpr int WR = Shape::WR, WC = Shape::WC;
+    using Acc = typename std::conditional<I8, intx4, floatx4>::type;
+    const int tile = blockIdx.x / WR, ta = blockIdx.x % WR;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = wave / Shape::NWC, wj = wave % Shape::NWC;
     int I, J;
     tile_at(g, tile, I, J);
-    Acc acc[NCT];
-    const Quad* in = reinterpret_cast<const Quad*>(g.partial) + (size_t)tile * (NRT * NCT * 4 * 256) + (size_t)ta * NCT * 4 * 256 + tid;
-    for (int z = 0; z < g.runs; ++z) {
+    Acc acc[WC];
+    const Acc* in = reinterpret_cast<const Acc*>(g.partial) + ((size_t)tile * WR + ta) * (WC * Shape::NT) + tid;
 #pragma unroll
-        for (int tb = 0; tb < NCT; ++tb)
+    for (int tb = 0; tb < WC; ++tb) acc[tb] = in[tb * Shape::NT];
+    for (int z = 1; z < g.runs; ++z) {
+        in += (size_t)g.tiles * (WR * WC * Shape::NT);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Quad q = in[(size_t)z * g.tiles * (NRT * NCT * 4 * 256) + (tb * 4 + i) * 256];
-                if (z == 0) { acc[tb][4 * i] = q.x; acc[tb][4 * i + 1] = q.y; acc[tb][4 * i + 2] = q.z; acc[tb][4 * i + 3] = q.w; }
-                else { acc[tb][4 * i] += q.x; acc[tb][4 * i + 1] += q.y; acc[tb][4 * i + 2] += q.z; acc[tb][4 * i + 3] += q.w; }
-            }
+        for (int tb = 0; tb < WC; ++tb) {
+            const Acc v = in[tb * Shape::NT];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[tb][i] += v[i];
+        }
     }
-    const int col = PAIR ? J * 32 * NCT + 16 * NCT * wj : J * 64 * NCT + 32 * NCT * wj;
-    epi.template apply<NCT>(I * 64 * NRT + 32 * NRT * wi + 32 * ta + 4 * half, col + l32, acc);
+    tile_apply<WC, PAIR>(epi, I * 64 * NRT + 16 * (wi * WR + ta) + (lane & 15), tile_column<WC, PAIR>(J * (PAIR ? 32 : 64) * NCT, wj, lane), acc);
 }
 
-// row of accumulation register i, for the first row that `apply` is given
-__device__ __forceinline__ int tile_row(int row0, int i) { return row0 + 8 * (i >> 2) + (i & 3); }
+// ---- what the epilogues store: four entries of a row from column s on, of `cols`
+__device__ __forceinline__ void tile_store(__bf16* p, int s, int cols, const float (&v)[4]) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    if (s + 4 <= cols) {
+        const bf16x4 o = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+        __builtin_memcpy(p, &o, 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (s + i < cols) p[i] = (__bf16)v[i];
+    }
+}
+__device__ __forceinline__ void tile_store(float* p, int s, int cols, const float (&v)[4]) {
+    if (s + 4 <= cols) {
+        __builtin_memcpy(p, v, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (s + i < cols) p[i] = v[i];
+    }
+}
+// four entries of a vector from column s on, zero beyond the end and for no vector
+__device__ __forceinline__ void tile_vector(const float* p, int s, int cols, float (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = p && s + i < cols ? p[s + i] : 0.f;
+}
 
 // Tile shape and runs of the least estimated time in cycles: rounds of 256 workgroups x (stages of a run + filling the ring) x the longer
-// of a stage's matrix instructions (32 cycles each) and its loads (about 40 bytes per cycle and compute unit), plus the pass that adds
-// the runs.  A run keeps at least 8 stages.
+// of a stage's matrix instructions and its loads (about 30 bytes per cycle and compute unit), plus the pass that adds the runs.  A run
+// keeps at least 4 stages.
 inline void tile_plan(TileProduct& g, bool pair) {
     static const int shapes[][2] = {{4, 4}, {2, 4}, {2, 2}, {1, 4}, {1, 2}};
     double best = 1e300;
@@ -266,10 +331,10 @@ inline void tile_plan(TileProduct& g, bool pair) {
         const int nrt = s[0], nct = s[1], tc = pair ? 32 * nct : 64 * nct;
         const int nrb = (g.R + 64 * nrt - 1) / (64 * nrt), ncb = (g.C + tc - 1) / tc;
         const long long tiles = (long long)nrb * ncb;
-        const double t_mfma = 64.0 * nrt * nct + 40.0, t_load = (nrt + nct) * 4096.0 / 40.0, t_stage = t_mfma > t_load ? t_mfma : t_load;
-        for (int runs = 1; runs <= 32 && (runs == 1 || (tiles * runs <= 512 && g.stages / runs >= 8)); ++runs) {
+        const double t_mfma = 128.0 * nrt * nct + 60.0, t_load = (nrt + nct) * 8192.0 / 30.0, t_stage = t_mfma > t_load ? t_mfma : t_load;
+        for (int runs = 1; runs <= 32 && (runs == 1 || (tiles * runs <= 512 && g.stages / runs >= 4)); ++runs) {
             const int spr = (g.stages + runs - 1) / runs, n = (g.stages + spr - 1) / spr;
-            double cost = (double)((tiles * n + 255) / 256) * (spr + 6.0) * t_stage;
+            double cost = (double)((tiles * n + 255) / 256) * (spr + 3.0) * t_stage;
             if (n > 1) cost += 6000.0 + 2.0 * n * tiles * (nrt * nct * 16384.0) / 4e12 * 2.1e9;
             if (cost < best * 0.999) {
                 best = cost;
@@ -282,14 +347,14 @@ inline size_t tile_partial_bytes(const TileProduct& g) {
     return g.runs > 1 ? align_up((size_t)g.runs * g.tiles * g.nrt * g.nct * 16384, 256) : 0;
 }
 
-template <bool I8, int NRT, int NCT, bool AKM, bool BKM, bool PAIR, class Epi>
+template <bool I8, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>
 fw_status tile_launch(const TileProduct& g, const Epi& epi, hipStream_t st) {
     const long long total = (long long)g.tiles * g.runs;
     if (total > (1 << 30)) return FW_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((tile_product_kernel<I8, NRT, NCT, AKM, BKM, PAIR, Epi>), dim3((unsigned)((total + 7) / 8 * 8)), dim3(256), 0, st, g, epi);
+    hipLaunchKernelGGL((tile_product_kernel<I8, NRT, NCT, NW, AKM, BKM, PAIR, Epi>), dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * NW), 0, st, g, epi);
     FW_LAUNCH_CHECK();
     if (g.runs > 1) {
-        hipLaunchKernelGGL((tile_runs_kernel<I8, NRT, NCT, PAIR, Epi>), dim3((unsigned)(g.tiles * NRT)), dim3(256), 0, st, g, epi);
+        hipLaunchKernelGGL((tile_runs_kernel<I8, NRT, NCT, NW, PAIR, Epi>), dim3((unsigned)(g.tiles * 2 * NRT)), dim3(64 * NW), 0, st, g, epi);
         FW_LAUNCH_CHECK();
     }
     return FW_OK;
@@ -297,11 +362,11 @@ fw_status tile_launch(const TileProduct& g, const Epi& epi, hipStream_t st) {
 
 template <bool I8, bool AKM, bool BKM, bool PAIR, class Epi>
 fw_status tile_product(const TileProduct& g, const Epi& epi, hipStream_t st) {
-    if (g.nrt == 4) return tile_launch<I8, 4, 4, AKM, BKM, PAIR>(g, epi, st);
-    if (g.nrt == 2 && g.nct == 4) return tile_launch<I8, 2, 4, AKM, BKM, PAIR>(g, epi, st);
-    if (g.nrt == 2) return tile_launch<I8, 2, 2, AKM, BKM, PAIR>(g, epi, st);
-    if (g.nct == 4) return tile_launch<I8, 1, 4, AKM, BKM, PAIR>(g, epi, st);
-    return tile_launch<I8, 1, 2, AKM, BKM, PAIR>(g, epi, st);
+    if (g.nrt == 4) return tile_launch<I8, 4, 4, 8, AKM, BKM, PAIR>(g, epi, st);
+    if (g.nrt == 2 && g.nct == 4) return tile_launch<I8, 2, 4, 8, AKM, BKM, PAIR>(g, epi, st);
+    if (g.nrt == 2) return tile_launch<I8, 2, 2, 8, AKM, BKM, PAIR>(g, epi, st);
+    if (g.nct == 4) return tile_launch<I8, 1, 4, 8, AKM, BKM, PAIR>(g, epi, st);
+    return tile_launch<I8, 1, 2, 4, AKM, BKM, PAIR>(g, epi, st);
 }
 
 }  // namespace fw
