@@ -66,12 +66,18 @@ __device__ __forceinline__ void dma16_from(const void* base, unsigned offset, vo
 }
 #pragma clang diagnostic pop
 
+template <int I, int N, class F> __device__ __forceinline__ void static_for(const F& f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        static_for<I + 1, N>(f);
+    }
+}
+
 template <int NRT, int NCT, int NW> struct TileShape {
     static constexpr int NWC = NW / 2;                          // wavefronts side by side
     static constexpr int WR = 2 * NRT, WC = 4 * NCT / NWC;      // 16 x 16 results of a wavefront, down and across
     static constexpr int NT = 64 * NW;
-    static constexpr int STAGE = 8192 * (NRT + NCT);            // bytes of a stage
-    static constexpr int NST = NRT + NCT >= 8 ? 2 : NRT + NCT == 3 ? 3 : NRT + NCT == 6 ? 3 : 2;
+    static constexpr int PA = 8192 * NRT, PB = 8192 * NCT;      // bytes of a stage of a panel
 };
 template <int WC, bool PAIR> __device__ __forceinline__ int tile_column(int panel, int wj, int lane) {
     return panel + wj * (PAIR ? 8 * WC : 16 * WC) + 4 * (lane >> 4);
@@ -88,13 +94,13 @@ __device__ __forceinline__ void tile_apply(const Epi& epi, int n, int s, const A
 
 // PAIR: the panel of B holds columns of b0 and the same columns of b1; results tb and tb + WC / 2 of a wavefront belong together.
 template <bool I8, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>
-__global__ __launch_bounds__(64 * NW, NW == 4 && NRT + NCT >= 8 ? 1 : 2) void tile_product_kernel(TileProduct g, Epi epi) {
+__global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g, Epi epi) {
     using Shape = TileShape<NRT, NCT, NW>;
-    constexpr int NST = Shape::NST, NWC = Shape::NWC, WR = Shape::WR, WC = Shape::WC;
+    constexpr int NWC = Shape::NWC, WR = Shape::WR, WC = Shape::WC;
     constexpr int LA = 8 * NRT / NW, LB = 8 * NCT / NW, NL = LA + LB;      // loads of a wavefront and stage
     constexpr int NF = WR + WC, NM = WR * WC;                             // fragments, matrix instructions
     using Acc = typename std::conditional<I8, intx4, floatx4>::type;
-    __shared__ __align__(1024) char lds[NST][Shape::STAGE];
+    __shared__ __align__(1024) char lds[3 * Shape::PA + 2 * Shape::PB];     // three stages of A, two of B
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / NWC, wj = wave % NWC;
@@ -109,64 +115,69 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && NRT + NCT >= 8 ? 1 : 2) void ti
     I = __builtin_amdgcn_readfirstlane(I); J = __builtin_amdgcn_readfirstlane(J);
     const int c0 = run * g.spr, cend = min(c0 + g.spr, g.stages);
 
-    // What this lane brings: of each panel a wavefront loads 1 KB pieces wave, wave + NW, ...; piece k comes from base[k] (the same for the
+    // What this lane brings: of each panel a wavefront loads 1 KB pieces wave, wave + NW, ..., from base_a or base_b (the same for the
     // wavefront) + the stage's offset + vof[k]
-    const char* base[NL];
+    const char *base_a, *base_b;
     unsigned vof[NL];
-    int lim[NL];                               // stages (of a part) below which the chunk lies inside the contraction
-    auto along = [&](const char* p, long long pitch, int row0, int rows, int k) __attribute__((always_inline)) {
-        const int c = (lane & 7) ^ (4 * (row0 >> 3 & 1) + (lane >> 4));       // row0 is a multiple of 8 from the panel's first on
-        row0 = min(row0, rows - 1);
-        base[k] = p + row0 * pitch;
-        vof[k] = (unsigned)(min(lane >> 3, rows - 1 - row0) * pitch) + 16 * c;
-        lim[k] = (g.chunks - c + 7) >> 3;
+    const int chunk = (lane & 7) ^ (4 * (wave & 1) + (lane >> 4));        // rows along the contraction: eight rows a piece, NW is even
+    auto along = [&](int row0, int rows, long long pitch, int first, int k) __attribute__((always_inline)) {
+        vof[k] = (unsigned)((min(row0 + (lane >> 3), rows - 1) - first) * pitch) + 16 * chunk;
     };
-    auto major = [&](auto N, const char* p, long long pitch, int tile0, int cols, int piece, int k) __attribute__((always_inline)) {
-        constexpr int CH = 8 * decltype(N)::value;               // chunks of a row of the panel
-        const int kr = piece * (64 / CH) + lane / CH;
-        const int c = (lane % CH) ^ (2 * pair_swizzle<decltype(N)::value>(kr));
-        base[k] = p;
-        vof[k] = (unsigned)(kr * pitch) + 16 * min(tile0 * CH + c, (cols + 7) / 8 - 1);
-        lim[k] = (g.klen - kr + 63) >> 6;
+    auto major = [&](auto N, long long pitch, int tile0, int cols, int k, int at) __attribute__((always_inline)) {
+        constexpr int CH = 8 * decltype(N)::value, RP = 64 / CH;          // chunks of a row of the panel, rows of a piece
+        static_assert(NW * RP % 16 == 0, "the permutation goes by four bits of the row and is the same for all pieces of a lane");
+        const int c = (lane % CH) ^ (2 * pair_swizzle<decltype(N)::value>(wave * RP + lane / CH));
+        vof[at] = (unsigned)(((wave + NW * k) * RP + lane / CH) * pitch) + 16 * min(tile0 * CH + c, (cols + 7) / 8 - 1);
     };
+    if constexpr (AKM) {
+        base_a = g.a;
 #pragma unroll
-    for (int k = 0; k < LA; ++k) {
-        const int piece = wave + NW * k;
-        if constexpr (AKM) major(std::integral_constant<int, NRT>(), g.a, g.apitch, I, g.R, piece, k);
-        else along(g.a, g.apitch, I * 64 * NRT + 8 * piece, g.R, k);
+        for (int k = 0; k < LA; ++k) major(std::integral_constant<int, NRT>(), g.apitch, I, g.R, k, k);
+    } else {
+        const int first = I * 64 * NRT;
+        base_a = g.a + first * g.apitch;
+#pragma unroll
+        for (int k = 0; k < LA; ++k) along(first + 8 * (wave + NW * k), g.R, g.apitch, first, k);
     }
+    if constexpr (BKM) {
+        base_b = g.b0;
 #pragma unroll
-    for (int k = 0; k < LB; ++k) {
-        const int piece = wave + NW * k;
-        if constexpr (BKM) major(std::integral_constant<int, NCT>(), g.b0, g.bpitch, J, g.C, piece, LA + k);
-        else if constexpr (PAIR) {
-            const int pr = 8 * piece, w = pr % (16 * WC);       // row of the panel, of its wavefront's part
-            const int col = J * 32 * NCT + pr / (16 * WC) * 8 * WC + w % (8 * WC);
-            along(w >= 8 * WC ? g.b1 : g.b0, g.bpitch, col, g.C, LA + k);
-        } else along(g.b0, g.bpitch, J * 64 * NCT + 8 * piece, g.C, LA + k);
+        for (int k = 0; k < LB; ++k) major(std::integral_constant<int, NCT>(), g.bpitch, J, g.C, k, LA + k);
+    } else {
+        const int first = J * (PAIR ? 32 : 64) * NCT;
+        const int w = 8 * wave % (16 * WC);                              // place in the wavefront's part of the panel, the same for all pieces
+        static_assert(!PAIR || 8 * NW % (16 * WC) == 0, "a wavefront brings columns of one matrix");
+        base_b = (PAIR && w >= 8 * WC ? g.b1 : g.b0) + first * g.bpitch;
+#pragma unroll
+        for (int k = 0; k < LB; ++k) {
+            const int pr = 8 * (wave + NW * k);
+            along(first + (PAIR ? pr / (16 * WC) * 8 * WC + w % (8 * WC) : pr), g.C, g.bpitch, first, LA + k);
+        }
     }
     const long long second = BKM ? g.b1 - g.b0 : 0;
     // stages that lie inside the contraction with all their chunks (of a part)
     const int whole = AKM || BKM ? g.klen >> 6 : g.chunks >> 3;
-    struct Stage { long long a, b; int c, cb; bool all; };
+    struct Stage { const char *a, *b; int c, cb; };
     auto stage_at = [&](int c) __attribute__((always_inline)) {
         Stage s;
         const bool two = BKM && c >= g.part;
         s.c = c; s.cb = two ? c - g.part : c;
-        s.a = AKM ? (long long)c * 64 * g.apitch : (long long)c * 128;
-        s.b = BKM ? (long long)s.cb * 64 * g.bpitch + (two ? second : 0) : (long long)c * 128;
-        s.all = c < cend && s.cb < whole;
+        s.a = base_a + (AKM ? (long long)c * 64 * g.apitch : (long long)c * 128);
+        s.b = base_b + (BKM ? (long long)s.cb * 64 * g.bpitch + (two ? second : 0) : (long long)c * 128);
         return s;
     };
-    auto load_one = [&](int buf, const Stage& s, int k) __attribute__((always_inline)) {      // k is a constant after unrolling
+    // ALL: the whole stage lies inside the contraction
+    auto load_one = [&](auto ALL, int to_buf, const Stage& s, int k) __attribute__((always_inline)) {      // k is a constant after unrolling
         const bool isa = k < LA;
-        void* to = &lds[buf][1024 * (wave + NW * (isa ? k : k - LA)) + (isa ? 0 : 8192 * NRT)];
-        const char* from = base[k] + (isa ? s.a : s.b);
-        if (s.all) {
-            dma16_from(from, vof[k], to);
+        void* to = &lds[to_buf + 1024 * (wave + NW * (isa ? k : k - LA))];
+        if constexpr (decltype(ALL)::value) {
+            dma16_from(isa ? s.a : s.b, vof[k], to);
         } else {
-            const bool inside = s.c < cend && (isa ? s.c : s.cb) < lim[k];
-            dma16(inside ? (const void*)(from + vof[k]) : (const void*)&tile_zero, to);
+            const int c = isa ? s.c : s.cb, RP = 8 / (isa ? NRT : NCT);
+            const bool major = isa ? AKM : BKM;
+            const bool inside = s.c < cend && (major ? 64 * c + (wave + NW * (isa ? k : k - LA)) * RP + lane / (64 / RP) < g.klen
+                                                     : 8 * c + chunk < g.chunks);
+            dma16(inside ? (const void*)((isa ? s.a : s.b) + vof[k]) : (const void*)&tile_zero, to);
         }
     };
 
@@ -183,11 +194,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && NRT + NCT >= 8 ? 1 : 2) void ti
     const int l16 = lane & 15, q = lane >> 4, kq = 8 * q + (l16 >> 2);       // kq + 4 and kq + 32 have the permutation of kq
     const int along_at = l16 * 128 + 16 * (q ^ (l16 >> 1));
     const int at_a = AKM ? kq * 128 * NRT + 32 * (wi * WR ^ pair_swizzle<NRT>(kq)) + 8 * (l16 & 3) : wi * WR * 2048 + along_at;
-    const int at_b = 8192 * NRT + (BKM ? kq * 128 * NCT + 32 * (wj * WC ^ pair_swizzle<NCT>(kq)) + 8 * (l16 & 3) : wj * WC * 2048 + along_at);
-    auto read_one = [&](int a, int b, int half, int f) __attribute__((always_inline)) {    // a, b: at_a and at_b in the stage's buffer
+    const int at_b = (BKM ? kq * 128 * NCT + 32 * (wj * WC ^ pair_swizzle<NCT>(kq)) + 8 * (l16 & 3) : wj * WC * 2048 + along_at);
+    auto read_one = [&](int a, int b, int half, int f) __attribute__((always_inline)) {    // a, b: at_a and at_b in the stage's buffers
         const bool isa = f < WR;
         const int r = isa ? f : f - WR;
-        const char* all = &lds[0][0];
+        const char* all = lds;
         if (isa ? AKM : BKM) {
             const int rowb = 128 * (isa ? NRT : NCT);
             const char* p = all + ((isa ? a : b) ^ (32 * r)) + 32 * half * rowb;
@@ -209,48 +220,61 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && NRT + NCT >= 8 ? 1 : 2) void ti
                                                                   __builtin_bit_cast(bf16x8, fr[half][ta]), acc[ta][tb], 0, 0, 0);
     };
 
-    // The loads of a wavefront complete in order: "at most those of NST - 2 stages outstanding" means that the stage before them has
-    // landed for it, the barrier extends that to all.  At the barrier in the middle of a stage every wavefront holds the stage's second
-    // half in registers, so its buffer is free for the stage NST further on.  Every stage issues the same number of loads (past the end
-    // they fetch zeros), which keeps the count valid.
-    for (int i = 0; i < NST; ++i) {
-        const Stage s = stage_at(c0 + i);
+    // At the barrier in the middle of stage c every wavefront holds the stage's second half in registers, so its buffers are free: in the
+    // half that follows the loads of B's stage c + 2 go out, in the half after that those of A's stage c + 3 (three buffers for A, two
+    // for B: what 160 KB hold for 256 x 256 results).  The loads of a wavefront complete in order; with those of A's stage c + 2
+    // outstanding all of stage c + 1 has landed for it, the barrier extends that to all.  Past the end the loads fetch zeros, which
+    // keeps their number the same.
+    auto load_panel = [&](auto ISA, int to_buf, int c) __attribute__((always_inline)) {
+        const Stage s = stage_at(c);
 #pragma unroll
-        for (int k = 0; k < NL; ++k) load_one(i, s, k);
-    }
-    FW_WAIT_VM((NST - 1) * NL);
+        for (int k = decltype(ISA)::value ? 0 : LA; k < (decltype(ISA)::value ? LA : NL); ++k) load_one(std::false_type(), to_buf, s, k);
+    };
+    constexpr int B0 = 3 * Shape::PA;
+    load_panel(std::true_type(), 0, c0);
+    load_panel(std::false_type(), B0, c0);
+    load_panel(std::true_type(), Shape::PA, c0 + 1);
+    load_panel(std::false_type(), B0 + Shape::PB, c0 + 1);
+    FW_WAIT_VM(NL);
     __builtin_amdgcn_s_barrier();
     FW_COMPILER_FENCE();
 #pragma unroll
-    for (int f = 0; f < NF; ++f) read_one(at_a, at_b, 0, f);
-    int sc = 0;
+    for (int f = 0; f < NF; ++f) read_one(at_a, B0 + at_b, 0, f);
     // the reads over the first three quarters of the matrix instructions (the last ones have to be back when the next half begins)
-    auto half_turn = [&](int ra, int rb, auto HALF, auto&& also) __attribute__((always_inline)) {
-        constexpr int half = decltype(HALF)::value;
-#pragma unroll
-        for (int m = 0; m < NM; ++m) {
+    auto half_turn = [&](int ra, int rb, auto HALF, auto ISA, auto ALL, int to_buf, const Stage& next) __attribute__((always_inline)) {
+        constexpr int half = decltype(HALF)::value, K0 = decltype(ISA)::value ? 0 : LA, KN = decltype(ISA)::value ? LA : LB;
+        static_for<0, NM>([&](auto M) __attribute__((always_inline)) {
+            constexpr int m = decltype(M)::value;
 #pragma unroll
             for (int r = 0; r < NF; ++r)
                 if (r * (3 * NM) / (4 * NF) == m) read_one(ra, rb, half ^ 1, r);
-            also(m);
+#pragma unroll
+            for (int k = 0; k < KN; ++k)
+                if (k * NM / KN + (NM > KN) == m) load_one(ALL, to_buf, next, K0 + k);
             multiply_one(half, m);
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
     };
-    for (int c = c0; c < cend; ++c) {
-        const Stage next = stage_at(c + NST);
-        const int sn = sc == NST - 1 ? 0 : sc + 1;
-        half_turn(at_a + sc * Shape::STAGE, at_b + sc * Shape::STAGE, std::integral_constant<int, 0>(), [](int) {});
+    int a0 = 0, b0 = B0;                         // the stage's buffers
+    int c = c0;
+    auto turn = [&](auto ALL) __attribute__((always_inline)) {
+        const int a1 = a0 == 2 * Shape::PA ? 0 : a0 + Shape::PA, a2 = a1 == 2 * Shape::PA ? 0 : a1 + Shape::PA;
+        const int b1 = 2 * B0 + Shape::PB - b0;
+        const Stage next = stage_at(c + 2);
+        half_turn(at_a + a0, at_b + b0, std::integral_constant<int, 0>(), std::true_type(), ALL, a2, next);
         FW_WAIT_LGKM0();
-        FW_WAIT_VM((NST - 2) * NL);
+        FW_WAIT_VM(LA);
         __builtin_amdgcn_s_barrier();
         FW_COMPILER_FENCE();
-        half_turn(at_a + sn * Shape::STAGE, at_b + sn * Shape::STAGE, std::integral_constant<int, 1>(), [&](int m) __attribute__((always_inline)) {
-#pragma unroll
-            for (int k = 0; k < NL; ++k)
-                if (k * NM / NL == m) load_one(sc, next, k);
-        });
-        sc = sn;
+        half_turn(at_a + a1, at_b + b1, std::integral_constant<int, 1>(), std::false_type(), ALL, b0, next);
+        a0 = a1; b0 = b1;
+        ++c;
+    };
+    while (c < cend) {
+        // stages up to `fast` ask for whole ones only
+        const int fast = min(cend, BKM && c + 2 >= g.part ? g.part + whole : min(whole, g.part)) - 2;
+        while (c < fast) turn(std::true_type());
+        turn(std::false_type());
     }
     FW_WAIT_VM(0);
     FW_WAIT_LGKM0();
@@ -366,7 +390,7 @@ fw_status tile_product(const TileProduct& g, const Epi& epi, hipStream_t st) {
     if (g.nrt == 2 && g.nct == 4) return tile_launch<I8, 2, 4, 8, AKM, BKM, PAIR>(g, epi, st);
     if (g.nrt == 2) return tile_launch<I8, 2, 2, 8, AKM, BKM, PAIR>(g, epi, st);
     if (g.nct == 4) return tile_launch<I8, 1, 4, 8, AKM, BKM, PAIR>(g, epi, st);
-    return tile_launch<I8, 1, 2, 4, AKM, BKM, PAIR>(g, epi, st);
+    return tile_launch<I8, 1, 2, 8, AKM, BKM, PAIR>(g, epi, st);
 }
 
 }  // namespace fw
