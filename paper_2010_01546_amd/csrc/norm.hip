@@ -4,76 +4,77 @@
 //   dx = rho w dy - h rho^3 / M sum(w dy h) + dh,                  dw = sum over rows of dy h rho
 //
 // Bound by memory: each input is read once and each output written once, a row stays in the registers of its group of threads (a
-// wavefront up to 2048 features, a workgroup beyond), 16 bytes per lane and access.
+// wavefront up to 2048 features, a workgroup beyond), 8 entries per lane and access.
 // The sums over a row are float64 (a row of 1e20s has a norm too, and the cost hides behind the loads).  So is q: rho falls out of
 // y / s = 127 h w / max |h w|, whose float32 rounding would put one value in 10^5 on the other side of a half.
 #include "fw_internal.h"
+#include "lane_sums.h"
+#include <type_traits>
 
 namespace fw {
 namespace {
 
-template <class T> struct Elem;
-template <> struct Elem<float> {
-    static __device__ __forceinline__ void load8(const float* p, float (&x)[8]) { __builtin_memcpy(x, p, 32); }
-    static __device__ __forceinline__ void store8(float* p, const float (&x)[8]) { __builtin_memcpy(p, x, 32); }
-    static __device__ __forceinline__ float get(const float* p) { return *p; }
-    static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
-    static __device__ __forceinline__ float held(float v) { return v; }
+// 8 entries of a row as they lie in memory (rows need not be 16-byte aligned)
+template <class T> struct Eight;
+template <> struct Eight<float> {
+    float v[8];
+    __device__ __forceinline__ float get(int i) const { return v[i]; }
+    static __device__ __forceinline__ float held(float x) { return x; }
 };
-template <> struct Elem<__bf16> {
-    static __device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
-        bf16x8 v;
-        __builtin_memcpy(&v, p, 16);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-    }
-    static __device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
-        bf16x8 v;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];
-        __builtin_memcpy(p, &v, 16);
-    }
-    static __device__ __forceinline__ float get(const __bf16* p) { return (float)*p; }
-    static __device__ __forceinline__ void put(__bf16* p, float v) { *p = (__bf16)v; }
-    static __device__ __forceinline__ float held(float v) { return (float)(__bf16)v; }
+template <> struct Eight<__bf16> {
+    unsigned v[4];
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
+    static __device__ __forceinline__ float held(float x) { return (float)(__bf16)x; }
 };
 
-// 8 entries of a row of which `left` remain (rows need not be 16-byte aligned); zero beyond the end
-template <class T> __device__ __forceinline__ void load8(const T* p, int left, float (&x)[8]) {
-    if (left >= 8) { Elem<T>::load8(p, x); return; }
+// How rows end.  WHOLE: a multiple of 8 entries.  RAGGED: the last lane's 8 entries are moved back to end with the row and `skip` of
+// them, which belong to the lane before, count as zero and are not stored.  SHORT: less than 8 entries, one lane, entry by entry.
+enum { WHOLE, RAGGED, SHORT };
+template <int END> struct Place {
+    int start, skip, count;       // entries skip .. count - 1 of the 8 from `start` on are this lane's
+    __device__ __forceinline__ Place(int m, int M) : start(END == RAGGED ? min(m, M - 8) : m), skip(END == RAGGED ? m - start : 0), count(END == SHORT ? M : 8) {}
+    __device__ __forceinline__ bool mine(int i) const { return END == WHOLE || (END == RAGGED ? i >= skip : i < count); }
+    template <class T> __device__ __forceinline__ void load(const T* row, Eight<T>& x) const {
+        if (END == SHORT) {
+            T e[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < left ? Elem<T>::get(p + i) : 0.f;
-}
-template <class T> __device__ __forceinline__ void store8(T* p, int left, const float (&x)[8]) {
-    if (left >= 8) { Elem<T>::store8(p, x); return; }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < left) Elem<T>::put(p + i, x[i]);
-}
-
-// over the G threads of a row's group; every thread gets the result
-template <int G, class Op> __device__ __forceinline__ double group_reduce(double v, double* red, Op op) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
-    if (G > 64) {
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();                     // the previous use of `red` is over
-        if ((threadIdx.x & 63) == 0) red[wave] = v;
-        __syncthreads();
-        v = red[0];
-#pragma unroll
-        for (int i = 1; i < G / 64; ++i) v = op(v, red[i]);
+            for (int i = 0; i < 8; ++i) e[i] = i < count ? row[i] : (T)0.f;
+            __builtin_memcpy(&x, e, sizeof(x));
+        } else {
+            __builtin_memcpy(&x, row + start, sizeof(x));
+        }
     }
+    template <class T> __device__ __forceinline__ void store(T* row, const float (&x)[8]) const {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = (T)x[i];
+        if (END == WHOLE || (END == RAGGED && skip == 0)) {
+            __builtin_memcpy(row + start, e, sizeof(e));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (mine(i)) row[start + i] = e[i];
+        }
+    }
+};
+
+// Sum and maximum over a wavefront, in every lane
+__device__ __forceinline__ double lanes_sum(double v) {
+    v = fold32(v, v);
+    v = fold16(v, v);
+    return sum16(v);
+}
+__device__ __forceinline__ double lanes_max(double v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmax(v, __shfl_xor(v, o, 64));
     return v;
 }
-struct Sum { __device__ double operator()(double a, double b) const { return a + b; } };
-struct Max { __device__ double operator()(double a, double b) const { return a > b ? a : b; } };
 
 // NORM: rows of the root mean square norm, otherwise the rows as they are (8 bits only)
-template <class T, int G, int NV, bool NORM>
+template <class T, int G, int NV, int END, bool NORM>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void rows_kernel(const T* X, const T* R, int N, int M, const float* __restrict__ w, float eps,
                                                                  T* H, T* Y, signed char* __restrict__ q, float* __restrict__ qs) {
-    __shared__ double red[16];
+    __shared__ double red[2][16];
     const int t = threadIdx.x % G;
     const long long row = (long long)blockIdx.x * (blockDim.x / G) + threadIdx.x / G;
     if (row >= N) return;                    // whole wavefronts, and only where a group is one
@@ -83,17 +84,19 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void rows_kernel(const T* X, con
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int m = 8 * (t + G * j);
-        if (m >= M) break;
-        load8(X + at + m, M - m, h[j]);
-        if (NORM && R) {
-            float r[8];
-            load8(R + at + m, M - m, r);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[j][i] = Elem<T>::held(h[j][i] + r[i]);
-        }
-        if (NORM) {
+        for (int i = 0; i < 8; ++i) h[j][i] = 0.f;
+        if (m >= M) continue;
+        const Place<END> p(m, M);
+        Eight<T> x, r;
+        p.load(X + at, x);
+        if (NORM && R) p.load(R + at, r);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ss += (double)h[j][i] * (double)h[j][i];
+        for (int i = 0; i < 8; ++i) {
+            float v = x.get(i);
+            if (NORM && R) v = Eight<T>::held(v + r.get(i));
+            h[j][i] = p.mine(i) ? v : 0.f;
+            if (NORM) ss += (double)h[j][i] * (double)h[j][i];
         }
     }
     double rho = 1.0;
@@ -102,22 +105,31 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void rows_kernel(const T* X, con
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int m = 8 * (t + G * j);
-                if (m < M) store8(H + at + m, M - m, h[j]);
+                if (m < M) Place<END>(m, M).store(H + at, h[j]);
             }
         }
-        ss = group_reduce<G>(ss, red, Sum());
+        ss = lanes_sum(ss);
+        if (G > 64) {
+            if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = ss;
+            __syncthreads();
+            ss = 0.0;
+#pragma unroll
+            for (int i = 0; i < G / 64; ++i) ss += red[0][i];
+        }
         rho = 1.0 / sqrt(ss / (double)M + (double)eps);
         if (Y) {
             const float rf = (float)rho;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int m = 8 * (t + G * j);
-                if (m >= M) break;
+                if (m >= M) continue;
+                const Place<END> p(m, M);
+                Eight<float> f;
+                if (w) p.load(w, f);
                 float y[8];
-                if (w) load8(w + m, M - m, y);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = h[j][i] * rf * (w ? y[i] : 1.f);
-                store8(Y + at + m, M - m, y);
+                for (int i = 0; i < 8; ++i) y[i] = h[j][i] * rf * (w ? f.get(i) : 1.f);
+                p.store(Y + at, y);
             }
         }
     }
@@ -126,134 +138,180 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void rows_kernel(const T* X, con
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int m = 8 * (t + G * j);
-            if (m >= M) break;
-            float f[8];
-            if (NORM && w) load8(w + m, M - m, f);
+            if (m >= M) continue;
+            const Place<END> p(m, M);
+            Eight<float> f;
+            if (NORM && w) p.load(w, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double a = fabs(NORM && w ? (double)h[j][i] * (double)f[i] : (double)h[j][i]);
+                const double a = fabs(NORM && w && p.mine(i) ? (double)h[j][i] * (double)f.get(i) : (double)h[j][i]);
                 top = fmax(top, a < __builtin_inf() ? a : __builtin_inf());   // NaN counts as infinite
             }
         }
-        top = group_reduce<G>(top, red, Max());
+        top = lanes_max(top);
+        if (G > 64) {
+            if ((threadIdx.x & 63) == 0) red[1][threadIdx.x >> 6] = top;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < G / 64; ++i) top = fmax(top, red[1][i]);
+        }
         const bool fine = top > 0.0 && top < __builtin_inf() && rho > 0.0;
         const double inv = fine ? 127.0 / top : 0.0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int m = 8 * (t + G * j);
-            if (m >= M) break;
-            float f[8];
-            if (NORM && w) load8(w + m, M - m, f);
+            if (m >= M) continue;
+            const Place<END> p(m, M);
+            Eight<float> f;
+            if (NORM && w) p.load(w, f);
             signed char b[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double a = NORM && w ? (double)h[j][i] * (double)f[i] : (double)h[j][i];
+                const double a = NORM && w ? (double)h[j][i] * (double)f.get(i) : (double)h[j][i];
                 b[i] = fine ? (signed char)(int)rint(a * inv) : (signed char)0;
             }
-            if (M - m >= 8) {
-                __builtin_memcpy(q + at + m, b, 8);
+            if (END == WHOLE || (END == RAGGED && p.skip == 0)) {
+                __builtin_memcpy(q + at + p.start, b, 8);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (i < M - m) q[at + m + i] = b[i];
+                    if (p.mine(i)) q[at + p.start + i] = b[i];
             }
         }
         if (t == 0) qs[row] = top == 0.0 && rho > 0.0 ? 0.f : fine ? (float)(rho * top / 127.0) : __builtin_nanf("");
     }
 }
 
-// Workgroups take rows in turn; each keeps the sums of its rows' dy h rho and leaves them in part[workgroup][M].
-template <class T, int G, int NV>
-__global__ __launch_bounds__(G < 256 ? 256 : G) void rms_grad_kernel(const T* __restrict__ H, int N, int M, const float* __restrict__ w, float eps,
-                                                                     const T* dY, const T* dH, T* dX, float* __restrict__ part) {
+// Workgroups take rows in turn; each keeps the sums of its rows' dy h rho and leaves them in part[workgroup][Mp].  The next row's h and dy
+// are asked for before this row's sums go round the wavefronts (a row of a workgroup waits for memory, then for its sums, then stores:
+// one after the other that took 136 us for 8192 x 4608 in bfloat16).
+template <class T, int G, int NV, int END>
+__global__ __launch_bounds__(G < 256 ? 256 : G) void rms_grad_kernel(const T* __restrict__ H, int N, int M, int Mp, const float* __restrict__ w,
+                                                                     float eps, const T* dY, const T* dH, T* dX, float* __restrict__ part) {
     constexpr int RB = G < 256 ? 256 / G : 1;
-    __shared__ double red[16];
+    __shared__ double red[2][16][2];
     __shared__ float acc[RB > 1 ? RB * 8 * G * NV : 1];
-    const int t = threadIdx.x % G, sub = threadIdx.x / G;
+    const int t = threadIdx.x % G, sub = threadIdx.x / G, wave = threadIdx.x >> 6;
     float sum[NV][8];
+    Eight<float> f[NV];
+    Eight<T> h[NV], v[NV], d[NV];
+    const long long step = (long long)gridDim.x * RB;
+    long long row = (long long)blockIdx.x * RB + sub;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+        const int m = 8 * (t + G * j);
+        const Place<END> p(m, M);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[j][i] = 0.f;
-    for (long long row = (long long)blockIdx.x * RB + sub; row < N; row += (long long)gridDim.x * RB) {
+        for (int i = 0; i < 8; ++i) { sum[j][i] = 0.f; f[j].v[i] = 1.f; }
+        h[j] = v[j] = d[j] = Eight<T>{};
+        if (m < M && w) p.load(w, f[j]);
+        if (m < M && row < N) {
+            p.load(H + (size_t)row * M, h[j]);
+            p.load(dY + (size_t)row * M, v[j]);
+        }
+    }
+    for (int turn = 0; row < N; row += step, turn ^= 1) {
         const size_t at = (size_t)row * M;
-        float h[NV][8], v[NV][8];
+        Eight<T> nh[NV], nv[NV];
         double ss = 0.0, dot = 0.0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int m = 8 * (t + G * j);
-            if (m >= M) break;
-            load8(H + at + m, M - m, h[j]);
-            load8(dY + at + m, M - m, v[j]);
-            float f[8];
-            if (w) load8(w + m, M - m, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                ss += (double)h[j][i] * (double)h[j][i];
-                dot += (double)h[j][i] * (w ? (double)v[j][i] * (double)f[i] : (double)v[j][i]);
+            const Place<END> p(m, M);
+            if (m < M && dH) p.load(dH + at, d[j]);
+            nh[j] = h[j]; nv[j] = v[j];
+            if (m < M && row + step < N) {
+                p.load(H + at + step * M, nh[j]);
+                p.load(dY + at + step * M, nv[j]);
             }
         }
-        ss = group_reduce<G>(ss, red, Sum());
-        dot = group_reduce<G>(dot, red, Sum());
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const Place<END> p(8 * (t + G * j), M);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double x = p.mine(i) ? (double)h[j].get(i) : 0.0;
+                ss += x * x;
+                dot += p.mine(i) ? x * (double)(v[j].get(i) * f[j].get(i)) : 0.0;
+            }
+        }
+        ss = lanes_sum(ss);
+        dot = lanes_sum(dot);
+        if (G > 64) {                            // two sets in turn: a set is written again only after the barrier of the next row
+            if ((threadIdx.x & 63) == 0) { red[turn][wave][0] = ss; red[turn][wave][1] = dot; }
+            __syncthreads();
+            ss = dot = 0.0;
+#pragma unroll
+            for (int i = 0; i < G / 64; ++i) { ss += red[turn][i][0]; dot += red[turn][i][1]; }
+        }
         const double rho = 1.0 / sqrt(ss / (double)M + (double)eps);
         const float rf = (float)rho, cf = (float)(rho * rho * rho * dot / (double)M);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int m = 8 * (t + G * j);
-            if (m >= M) break;
-            if (part) {
+            float x[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[j][i] += v[j][i] * (h[j][i] * rf);
+            for (int i = 0; i < 8; ++i) {
+                const float hv = h[j].get(i), vv = v[j].get(i);
+                sum[j][i] += vv * (hv * rf);
+                x[i] = rf * (vv * f[j].get(i)) - hv * cf;
+                if (dH) x[i] += d[j].get(i);
             }
-            if (dX) {
-                float f[8], d[8];
-                if (w) load8(w + m, M - m, f);
-                if (dH) load8(dH + at + m, M - m, d);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float x = rf * (w ? v[j][i] * f[i] : v[j][i]) - h[j][i] * cf;
-                    v[j][i] = dH ? x + d[i] : x;
-                }
-                store8(dX + at + m, M - m, v[j]);
-            }
+            if (dX && m < M) Place<END>(m, M).store(dX + at, x);
+            h[j] = nh[j]; v[j] = nv[j];
         }
     }
     if (!part) return;
     if (RB > 1) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j) {
+            const Place<END> p(8 * (t + G * j), M);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[(sub * NV + j) * 8 * G + 8 * t + i] = sum[j][i];
+            for (int i = 0; i < 8; ++i)
+                if (8 * (t + G * j) < M && p.mine(i)) acc[sub * NV * 8 * G + p.start + i] = sum[j][i];
+        }
         __syncthreads();
         for (int m = threadIdx.x; m < M; m += blockDim.x) {
             float s = 0.f;
 #pragma unroll
             for (int r = 0; r < RB; ++r) s += acc[r * NV * 8 * G + m];
-            part[(size_t)blockIdx.x * M + m] = s;
+            part[(size_t)blockIdx.x * Mp + m] = s;
         }
     } else {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int m = 8 * (t + G * j);
-            if (m < M) store8(part + (size_t)blockIdx.x * M + m, M - m, sum[j]);
+            if (m < M) Place<END>(m, M).store(part + (size_t)blockIdx.x * Mp, sum[j]);
         }
     }
 }
 
-// dw[m] = sum of the workgroups' partial sums, in a fixed order: 16 slices of them, then the slices
-__global__ __launch_bounds__(1024) void column_sum_kernel(const float* __restrict__ part, int P, int M, float* __restrict__ dw) {
-    __shared__ float red[16][64];
-    const int m = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
-    float s = 0.f;
+// dw[m] = sum of the workgroups' partial sums, in a fixed order: 64 slices of them, then the slices.  16 columns of a workgroup.
+__global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict__ part, int P, int M, int Mp, float* __restrict__ dw) {
+    __shared__ float red[64][17];
+    const int q = threadIdx.x & 3, slice = threadIdx.x >> 2, m = blockIdx.x * 16 + 4 * q;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (m < M)
-        for (int p = slice; p < P; p += 16) s += part[(size_t)p * M + m];
-    red[slice][threadIdx.x & 63] = s;
+#pragma unroll 4
+        for (int p = slice; p < P; p += 64) {
+            const float4 v = *reinterpret_cast<const float4*>(part + (size_t)p * Mp + m);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+    red[slice][4 * q] = s.x; red[slice][4 * q + 1] = s.y; red[slice][4 * q + 2] = s.z; red[slice][4 * q + 3] = s.w;
     __syncthreads();
-    if (slice == 0 && m < M) {
-        float v = 0.f;
+    // 16 threads of a column add four slices each, then one of them adds those
+    const int c = threadIdx.x & 15, part16 = threadIdx.x >> 4;
+    float v = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v += red[i][threadIdx.x];
-        dw[m] = v;
+    for (int i = 0; i < 4; ++i) v += red[4 * part16 + i][c];
+    __syncthreads();
+    red[part16][c] = v;
+    __syncthreads();
+    if (threadIdx.x < 16 && blockIdx.x * 16 + c < M) {
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v += red[i][c];
+        dw[blockIdx.x * 16 + c] = v;
     }
 }
 
@@ -261,7 +319,27 @@ inline int rows_per_group(int M) { return M <= 2048 ? 4 : 1; }
 inline int grad_blocks(int N, int M) {
     const int rb = rows_per_group(M);
     const long long b = ((long long)N + rb - 1) / rb;
-    return (int)(b < 1024 ? b : 1024);
+    return (int)(b < 512 ? b : 512);
+}
+inline int up4(int m) { return (m + 3) / 4 * 4; }
+
+// calls f(threads of a row, accesses of each, how rows end): as few accesses of 8 entries as hold the row
+template <class F> void with_shape(int M, const F& f) {
+    auto with_end = [&](auto G, auto NV) {
+        if (M % 8 == 0) f(G, NV, std::integral_constant<int, WHOLE>());
+        else f(G, NV, std::integral_constant<int, RAGGED>());
+    };
+    using std::integral_constant;
+    if (M < 8) f(integral_constant<int, 64>(), integral_constant<int, 1>(), integral_constant<int, SHORT>());
+    else if (M <= 512) with_end(integral_constant<int, 64>(), integral_constant<int, 1>());
+    else if (M <= 1024) with_end(integral_constant<int, 64>(), integral_constant<int, 2>());
+    else if (M <= 1536) with_end(integral_constant<int, 64>(), integral_constant<int, 3>());
+    else if (M <= 2048) with_end(integral_constant<int, 64>(), integral_constant<int, 4>());
+    else if (M <= 4096) with_end(integral_constant<int, 256>(), integral_constant<int, 2>());
+    else if (M <= 6144) with_end(integral_constant<int, 256>(), integral_constant<int, 3>());
+    else if (M <= 8192) with_end(integral_constant<int, 512>(), integral_constant<int, 2>());
+    else if (M <= 16384) with_end(integral_constant<int, 1024>(), integral_constant<int, 2>());
+    else with_end(integral_constant<int, 1024>(), integral_constant<int, 4>());
 }
 
 template <class T, bool NORM>
@@ -269,16 +347,12 @@ fw_status rows_launch(const void* X, const void* R, int N, int M, const float* w
                       hipStream_t st) {
     const int rb = rows_per_group(M);
     const dim3 grid((unsigned)(((long long)N + rb - 1) / rb));
-    const T *x = reinterpret_cast<const T*>(X), *r = reinterpret_cast<const T*>(R);
-    T *h = reinterpret_cast<T*>(H), *y = reinterpret_cast<T*>(Y);
-#define FW_ROWS(G, NV) hipLaunchKernelGGL((rows_kernel<T, G, NV, NORM>), grid, dim3(G < 256 ? 256 : G), 0, st, x, r, N, M, w, eps, h, y, q, qs)
-    if (M <= 512) FW_ROWS(64, 1);
-    else if (M <= 1024) FW_ROWS(64, 2);
-    else if (M <= 2048) FW_ROWS(64, 4);
-    else if (M <= 8192) FW_ROWS(256, 4);
-    else if (M <= 16384) FW_ROWS(512, 4);
-    else FW_ROWS(1024, 4);
-#undef FW_ROWS
+    with_shape(M, [&](auto G, auto NV, auto END) {
+        constexpr int g = decltype(G)::value;
+        hipLaunchKernelGGL((rows_kernel<T, g, decltype(NV)::value, decltype(END)::value, NORM>), grid, dim3(g < 256 ? 256 : g), 0, st,
+                           reinterpret_cast<const T*>(X), reinterpret_cast<const T*>(R), N, M, w, eps, reinterpret_cast<T*>(H),
+                           reinterpret_cast<T*>(Y), q, qs);
+    });
     FW_LAUNCH_CHECK();
     return FW_OK;
 }
@@ -287,16 +361,12 @@ template <class T>
 fw_status grad_launch(const void* H, int N, int M, const float* w, float eps, const void* dY, const void* dH, void* dX, float* part,
                       hipStream_t st) {
     const dim3 grid(grad_blocks(N, M));
-    const T *h = reinterpret_cast<const T*>(H), *dy = reinterpret_cast<const T*>(dY), *dh = reinterpret_cast<const T*>(dH);
-    T* dx = reinterpret_cast<T*>(dX);
-#define FW_GRAD(G, NV) hipLaunchKernelGGL((rms_grad_kernel<T, G, NV>), grid, dim3(G < 256 ? 256 : G), 0, st, h, N, M, w, eps, dy, dh, dx, part)
-    if (M <= 512) FW_GRAD(64, 1);
-    else if (M <= 1024) FW_GRAD(64, 2);
-    else if (M <= 2048) FW_GRAD(64, 4);
-    else if (M <= 8192) FW_GRAD(256, 4);
-    else if (M <= 16384) FW_GRAD(512, 4);
-    else FW_GRAD(1024, 4);
-#undef FW_GRAD
+    with_shape(M, [&](auto G, auto NV, auto END) {
+        constexpr int g = decltype(G)::value;
+        hipLaunchKernelGGL((rms_grad_kernel<T, g, decltype(NV)::value, decltype(END)::value>), grid, dim3(g < 256 ? 256 : g), 0, st,
+                           reinterpret_cast<const T*>(H), N, M, up4(M), w, eps, reinterpret_cast<const T*>(dY), reinterpret_cast<const T*>(dH),
+                           reinterpret_cast<T*>(dX), part);
+    });
     FW_LAUNCH_CHECK();
     return FW_OK;
 }
@@ -314,7 +384,7 @@ fw_status int8_rows(const void* X, fw_dtype dt, int N, int M, signed char* q, fl
                          : rows_launch<float, false>(X, nullptr, N, M, nullptr, 0.f, nullptr, nullptr, q, qs, st);
 }
 
-size_t rms_norm_grad_workspace_bytes(int N, int M) { return align_up((size_t)grad_blocks(N, M) * M * sizeof(float), 256); }
+size_t rms_norm_grad_workspace_bytes(int N, int M) { return align_up((size_t)grad_blocks(N, M) * up4(M) * sizeof(float), 256); }
 
 fw_status rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float* w, float eps, const void* dY, const void* dH, void* dX,
                         float* dw, void* ws, hipStream_t st) {
@@ -322,7 +392,7 @@ fw_status rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float* w
     const fw_status rc = dt == FW_BF16 ? grad_launch<__bf16>(H, N, M, w, eps, dY, dH, dX, part, st)
                                        : grad_launch<float>(H, N, M, w, eps, dY, dH, dX, part, st);
     if (rc != FW_OK || !dw) return rc;
-    hipLaunchKernelGGL(column_sum_kernel, dim3((M + 63) / 64), dim3(1024), 0, st, part, grad_blocks(N, M), M, dw);
+    hipLaunchKernelGGL(column_sum_kernel, dim3((M + 15) / 16), dim3(256), 0, st, part, grad_blocks(N, M), M, up4(M), dw);
     FW_LAUNCH_CHECK();
     return FW_OK;
 }
