@@ -65,9 +65,27 @@ __device__ __forceinline__ double lanes_sum(double v) {
     return sum16(v);
 }
 __device__ __forceinline__ double lanes_max(double v) {
+    union { double d; unsigned i[2]; } x, y;
+    x.d = v; y.d = v;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmax(v, __shfl_xor(v, o, 64));
-    return v;
+    for (int k = 0; k < 2; ++k) {
+        const auto r = __builtin_amdgcn_permlane32_swap(x.i[k], y.i[k], false, false);
+        x.i[k] = r[0]; y.i[k] = r[1];
+    }
+    x.d = y.d = fmax(x.d, y.d);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x.i[k], y.i[k], false, false);
+        x.i[k] = r[0]; y.i[k] = r[1];
+    }
+    x.d = fmax(x.d, y.d);
+#define FW_MAX16(c) y.i[0] = __builtin_amdgcn_update_dpp(0, x.i[0], c, 0xf, 0xf, true); y.i[1] = __builtin_amdgcn_update_dpp(0, x.i[1], c, 0xf, 0xf, true); x.d = fmax(x.d, y.d)
+    FW_MAX16(0xB1);      // lanes 1,0,3,2
+    FW_MAX16(0x4E);      // lanes 2,3,0,1
+    FW_MAX16(0x141);     // half of 16 mirrored
+    FW_MAX16(0x140);     // 16 mirrored
+#undef FW_MAX16
+    return x.d;
 }
 
 // NORM: rows of the root mean square norm, otherwise the rows as they are (8 bits only)
@@ -79,107 +97,83 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void rows_kernel(const T* X, con
     const long long row = (long long)blockIdx.x * (blockDim.x / G) + threadIdx.x / G;
     if (row >= N) return;                    // whole wavefronts, and only where a group is one
     const size_t at = (size_t)row * M;
+    const bool eight = !NORM || q;
     float h[NV][8];
-    double ss = 0.0;
+    Eight<float> f[NV];
+    double ss = 0.0, top = 0.0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int m = 8 * (t + G * j);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[j][i] = 0.f;
+        for (int i = 0; i < 8; ++i) { h[j][i] = 0.f; f[j].v[i] = 1.f; }
         if (m >= M) continue;
         const Place<END> p(m, M);
         Eight<T> x, r;
         p.load(X + at, x);
         if (NORM && R) p.load(R + at, r);
+        if (NORM && w) p.load(w, f[j]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float v = x.get(i);
             if (NORM && R) v = Eight<T>::held(v + r.get(i));
             h[j][i] = p.mine(i) ? v : 0.f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int m = 8 * (t + G * j);
+        const Place<END> p(m, M);
+        if (NORM && H && m < M) p.store(H + at, h[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
             if (NORM) ss += (double)h[j][i] * (double)h[j][i];
-        }
-    }
-    double rho = 1.0;
-    if (NORM) {
-        if (H) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int m = 8 * (t + G * j);
-                if (m < M) Place<END>(m, M).store(H + at, h[j]);
-            }
-        }
-        ss = lanes_sum(ss);
-        if (G > 64) {
-            if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = ss;
-            __syncthreads();
-            ss = 0.0;
-#pragma unroll
-            for (int i = 0; i < G / 64; ++i) ss += red[0][i];
-        }
-        rho = 1.0 / sqrt(ss / (double)M + (double)eps);
-        if (Y) {
-            const float rf = (float)rho;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int m = 8 * (t + G * j);
-                if (m >= M) continue;
-                const Place<END> p(m, M);
-                Eight<float> f;
-                if (w) p.load(w, f);
-                float y[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = h[j][i] * rf * (w ? f.get(i) : 1.f);
-                p.store(Y + at, y);
-            }
-        }
-    }
-    if (!NORM || q) {
-        double top = 0.0;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int m = 8 * (t + G * j);
-            if (m >= M) continue;
-            const Place<END> p(m, M);
-            Eight<float> f;
-            if (NORM && w) p.load(w, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const double a = fabs(NORM && w && p.mine(i) ? (double)h[j][i] * (double)f.get(i) : (double)h[j][i]);
+            if (eight) {
+                const double a = fabs(NORM && p.mine(i) ? (double)h[j][i] * (double)f[j].v[i] : (double)h[j][i]);
                 top = fmax(top, a < __builtin_inf() ? a : __builtin_inf());   // NaN counts as infinite
             }
         }
-        top = lanes_max(top);
-        if (G > 64) {
-            if ((threadIdx.x & 63) == 0) red[1][threadIdx.x >> 6] = top;
-            __syncthreads();
+    }
+    if (NORM) ss = lanes_sum(ss);
+    if (eight) top = lanes_max(top);
+    if (G > 64) {
+        if ((threadIdx.x & 63) == 0) { red[0][threadIdx.x >> 6] = ss; red[1][threadIdx.x >> 6] = top; }
+        __syncthreads();
+        ss = 0.0;
 #pragma unroll
-            for (int i = 0; i < G / 64; ++i) top = fmax(top, red[1][i]);
-        }
-        const bool fine = top > 0.0 && top < __builtin_inf() && rho > 0.0;
-        const double inv = fine ? 127.0 / top : 0.0;
+        for (int i = 0; i < G / 64; ++i) { ss += red[0][i]; top = fmax(top, red[1][i]); }
+    }
+    const double rho = NORM ? 1.0 / sqrt(ss / (double)M + (double)eps) : 1.0;
+    if (NORM && Y) {
+        const float rf = (float)rho;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int m = 8 * (t + G * j);
-            if (m >= M) continue;
-            const Place<END> p(m, M);
-            Eight<float> f;
-            if (NORM && w) p.load(w, f);
-            signed char b[8];
+            float y[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const double a = NORM && w ? (double)h[j][i] * (double)f.get(i) : (double)h[j][i];
-                b[i] = fine ? (signed char)(int)rint(a * inv) : (signed char)0;
-            }
-            if (END == WHOLE || (END == RAGGED && p.skip == 0)) {
-                __builtin_memcpy(q + at + p.start, b, 8);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (p.mine(i)) q[at + p.start + i] = b[i];
-            }
+            for (int i = 0; i < 8; ++i) y[i] = h[j][i] * rf * f[j].v[i];
+            if (m < M) Place<END>(m, M).store(Y + at, y);
         }
-        if (t == 0) qs[row] = top == 0.0 && rho > 0.0 ? 0.f : fine ? (float)(rho * top / 127.0) : __builtin_nanf("");
     }
+    if (!eight) return;
+    const bool fine = top > 0.0 && top < __builtin_inf() && rho > 0.0;
+    const double inv = fine ? 127.0 / top : 0.0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int m = 8 * (t + G * j);
+        if (m >= M) continue;
+        const Place<END> p(m, M);
+        signed char b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = fine ? (signed char)(int)rint((double)h[j][i] * (double)f[j].v[i] * inv) : (signed char)0;
+        if (END == WHOLE || (END == RAGGED && p.skip == 0)) {
+            __builtin_memcpy(q + at + p.start, b, 8);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (p.mine(i)) q[at + p.start + i] = b[i];
+        }
+    }
+    if (t == 0) qs[row] = top == 0.0 && rho > 0.0 ? 0.f : fine ? (float)(rho * top / 127.0) : __builtin_nanf("");
 }
 
 // Workgroups take rows in turn; each keeps the sums of its rows' dy h rho and leaves them in part[workgroup][Mp].  The next row's h and dy
