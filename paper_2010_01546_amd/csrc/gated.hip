@@ -8,7 +8,9 @@
 // over the rows of both weight matrices, and [dWg; dWu] = D^T X.  Operands that are contraction-major in memory are turned on the
 // way out of LDS, not in memory.  mu is taken out of the sums: D^T (X - 1 mu^T) = D^T X - (D^T 1) mu^T, with D^T 1 summed from the
 // rounded D, so that the identity is exact but for float32 sums.
-// float32: products with float32 accuracy on the bfloat16 matrix cores (gemm_planes.hip), operands transposed in the workspace.
+// float32: the same products with every operand as three bfloat16 planes (tile_product.h), split in one pass over X and the weights, D
+// when it is formed.  X is centred on mu as it is split.
+// float32 with few rows: the weights are read once as they are, each by one wavefront (few_rows_kernel).
 #include "fw_internal.h"
 #include "tile_product.h"
 
@@ -43,14 +45,29 @@ template <class F> __device__ __forceinline__ void with_activation(int act, cons
     else f(std::integral_constant<int, FW_ACT_RELU>());
 }
 
-// ---- epilogues of the bfloat16 products: four entries of a row
-struct GateEpilogue {
-    __bf16* H;
+// ---- epilogues: four entries of a row.  FIX (float32 planes): entries that are not finite are computed once more.
+__device__ __forceinline__ bool all_finite(const floatx4& v) {
+    return fabsf(v[0]) <= 3.402823466e38f && fabsf(v[1]) <= 3.402823466e38f && fabsf(v[2]) <= 3.402823466e38f && fabsf(v[3]) <= 3.402823466e38f;
+}
+template <class T> struct GateEpilogue {
+    static constexpr bool FIX = std::is_same<T, float>::value;
+    T* H;
     float* Z;
     const float *bg, *bu;
     int N, S, act;
-    __device__ __forceinline__ void apply(int n, int s, const floatx4& gate, const floatx4& up) const {
+    const float *X, *Wg, *Wu;             // FIX: the operands as they were
+    int M;
+    __device__ __noinline__ float dot(int n, int s, bool up) const {
+        const float *x = X + (size_t)n * M, *w = (up ? Wu : Wg) + (size_t)s * M;
+        float v = 0.f;
+        for (int m = 0; m < M; ++m) v = fmaf(x[m], w[m], v);
+        return v;
+    }
+    __device__ __forceinline__ void apply(int n, int s, floatx4 gate, floatx4 up) const {
         if (n >= N || s >= S) return;
+        if (FIX && !(all_finite(gate) && all_finite(up))) {
+            for (int i = 0; i < 4 && s + i < S; ++i) { gate[i] = dot(n, s + i, false); up[i] = dot(n, s + i, true); }
+        }
         float b[4], c[4], h[4];
         tile_vector(bg, s, S, b);
         tile_vector(bu, s, S, c);
@@ -73,22 +90,50 @@ struct GateEpilogue {
         }
     }
 };
-struct RowsEpilogue {                     // dX
-    __bf16* out;
+// what the float32 gradients are computed from once more
+struct GradInputs { const float *X, *Wg, *Wu, *Z, *dH, *mu; int N, M, S; };
+template <class T> struct RowsEpilogue {                     // dX
+    static constexpr bool FIX = std::is_same<T, float>::value;
+    T* out;
     int N, M;
-    __device__ __forceinline__ void apply(int n, int m, const floatx4& acc) const {
+    GradInputs in;
+    __device__ __noinline__ float dot(int n, int m) const {
+        float v = 0.f;
+        for (int s = 0; s < in.S; ++s) {
+            const size_t e = (size_t)n * in.S + s, w = (size_t)s * M + m;
+            v = fmaf(in.dH[e] * in.Z[e], in.Wg[w], v);
+            v = fmaf(in.dH[e] * in.Z[(size_t)N * in.S + e], in.Wu[w], v);
+        }
+        return v;
+    }
+    __device__ __forceinline__ void apply(int n, int m, floatx4 acc) const {
         if (n >= N || m >= M) return;
+        if (FIX && !all_finite(acc))
+            for (int i = 0; i < 4 && m + i < M; ++i) acc[i] = dot(n, m + i);
         const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
         tile_store(out + (size_t)n * M + m, m, M, v);
     }
 };
-struct WeightsEpilogue {                  // rows below Sp are the gate's, the others the up projection's
-    __bf16 *dWg, *dWu;
-    const float *sums, *mu;
+template <class T> struct WeightsEpilogue {                  // rows below Sp are the gate's, the others the up projection's
+    static constexpr bool FIX = std::is_same<T, float>::value;
+    T *dWg, *dWu;
+    const float *sums, *mu;               // mu: taken out here (bfloat16), or null
     int S, Sp, M;
-    __device__ __forceinline__ void apply(int r, int m, const floatx4& acc) const {
+    GradInputs in;
+    __device__ __noinline__ float dot(int s, bool up, int m) const {
+        const float c = in.mu ? in.mu[m] : 0.f;
+        float v = 0.f;
+        for (int n = 0; n < in.N; ++n) {
+            const size_t e = (size_t)n * S + s;
+            v = fmaf(in.dH[e] * in.Z[(up ? (size_t)in.N * S : 0) + e], in.X[(size_t)n * M + m] - c, v);
+        }
+        return v;
+    }
+    __device__ __forceinline__ void apply(int r, int m, floatx4 acc) const {
         const int s = r >= Sp ? r - Sp : r;
         if (s >= S || m >= M) return;
+        if (FIX && !all_finite(acc))
+            for (int i = 0; i < 4 && m + i < M; ++i) acc[i] = dot(s, r >= Sp, m + i);
         float v[4] = {acc[0], acc[1], acc[2], acc[3]};
         if (mu) {
             const float d = sums[r];
@@ -102,18 +147,94 @@ struct WeightsEpilogue {                  // rows below Sp are the gate's, the o
 };
 
 // ---- elementwise passes
-// float32: g and u [2][N][S] before the biases -> H, Z
-__global__ __launch_bounds__(256) void gate_kernel(const float* __restrict__ gu, size_t n, int S, const float* __restrict__ bg,
-                                                   const float* __restrict__ bu, int act, float* __restrict__ H, float* __restrict__ Z) {
-    for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (size_t)gridDim.x * 256) {
-        const int s = (int)(e % S);
-        const float g = gu[e] + (bg ? bg[s] : 0.f), u = gu[n + e] + (bu ? bu[s] : 0.f);
-        with_activation(act, [&](auto ACT) {
+// float32, up to FEW rows: a wavefront takes the two weight rows of an output, NR rows of X at a time (from the caches: all wavefronts read
+// the same ones).
+constexpr int FEW = 16;
+template <int NR>
+__global__ __launch_bounds__(256) void few_rows_kernel(const float* __restrict__ X, int N, int M, int S, const float* __restrict__ Wg,
+                                                       const float* __restrict__ Wu, GateEpilogue<float> epi) {
+    const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6), n0 = blockIdx.y * NR;
+    if (s >= S) return;
+    const float *wg = Wg + (size_t)s * M, *wu = Wu + (size_t)s * M;
+    float g[NR], u[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) g[r] = u[r] = 0.f;
+    const int whole = M / 256 * 256;
+#pragma unroll 2
+    for (int m = 4 * lane; m < whole; m += 256) {
+        float4 a, b;
+        __builtin_memcpy(&a, wg + m, 16);
+        __builtin_memcpy(&b, wu + m, 16);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            float4 x;
+            __builtin_memcpy(&x, X + (size_t)min(n0 + r, N - 1) * M + m, 16);
+            g[r] = fmaf(x.x, a.x, fmaf(x.y, a.y, fmaf(x.z, a.z, fmaf(x.w, a.w, g[r]))));
+            u[r] = fmaf(x.x, b.x, fmaf(x.y, b.y, fmaf(x.z, b.z, fmaf(x.w, b.w, u[r]))));
+        }
+    }
+    for (int m = whole + lane; m < M; m += 64) {
+        const float a = wg[m], b = wu[m];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const float x = X[(size_t)min(n0 + r, N - 1) * M + m];
+            g[r] = fmaf(x, a, g[r]);
+            u[r] = fmaf(x, b, u[r]);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < NR; ++r) { g[r] = wave_sum(g[r]); u[r] = wave_sum(u[r]); }
+    if (lane) return;
+    with_activation(epi.act, [&](auto ACT) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            if (n0 + r >= N) break;
+            const float gv = g[r] + (epi.bg ? epi.bg[s] : 0.f), uv = u[r] + (epi.bu ? epi.bu[s] : 0.f);
             float a, da;
-            activation<decltype(ACT)::value>(g, a, da);
-            H[e] = a * u;
-            if (Z) { Z[e] = u * da; Z[n + e] = a; }
-        });
+            activation<decltype(ACT)::value>(gv, a, da);
+            const size_t e = (size_t)(n0 + r) * S + s;
+            epi.H[e] = a * uv;
+            if (epi.Z) { epi.Z[e] = uv * da; epi.Z[(size_t)N * S + e] = a; }
+        }
+    });
+}
+
+// three bfloat16 planes of a float32 number
+__device__ __forceinline__ void planes_of(float x, __bf16& h, __bf16& m, __bf16& l) {
+    h = (__bf16)x;
+    const float r = x - (float)h;
+    m = (__bf16)r;
+    l = (__bf16)(r - (float)m);
+}
+
+// float32 matrices to planes [3][Rp][Mp], zeros past R and M; mu: taken out of the rows, or null.  The matrix goes by blockIdx.y.
+struct Split { const float* in[3]; __bf16* out[3]; int R[3], Rp[3]; const float* mu[3]; };
+__global__ __launch_bounds__(256) void split_planes_kernel(Split s, int M, int Mp) {
+    const int k = blockIdx.y, c8 = Mp / 8, R = s.R[k];
+    const size_t n8 = (size_t)s.Rp[k] * c8, plane = n8 * 8;
+    const float* mu = s.mu[k];
+    for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < n8; e += (size_t)gridDim.x * 256) {
+        const size_t r = e / c8;
+        const int m = 8 * (int)(e - r * c8);
+        float x[8];
+        const float* p = s.in[k] + r * M + m;
+        if (r < R && m + 8 <= M) {
+            __builtin_memcpy(x, p, 32);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = r < R && m + i < M ? p[i] : 0.f;
+        }
+        bf16x8 h, mm, l;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            __bf16 a, b, c;
+            planes_of(mu && r < R && m + i < M ? x[i] - mu[m + i] : x[i], a, b, c);
+            h[i] = a; mm[i] = b; l[i] = c;
+        }
+        bf16x8* o = reinterpret_cast<bf16x8*>(s.out[k]) + e;
+        o[0] = h;
+        o[plane / 8] = mm;
+        o[plane / 4] = l;
     }
 }
 
@@ -131,30 +252,47 @@ __device__ __forceinline__ void store4(__bf16* p, float (&x)[4]) {     // x: as 
     for (int i = 0; i < 4; ++i) { v[i] = (__bf16)x[i]; x[i] = (float)v[i]; }
     __builtin_memcpy(p, &v, 8);
 }
-__device__ __forceinline__ void store4(float* p, float (&x)[4]) { __builtin_memcpy(p, x, 16); }
 
 constexpr int GG_ROWS = 64;      // rows of a workgroup: 16 for each of its four wavefronts, 256 columns
-// D[n] = [dg | du] of row n, each Sp wide (zeros past S); part[block of rows][2 Sp]: sums over the block's rows, or null
+// D[n] = [dg | du] of row n, each Sp wide (zeros past S), float32 as three planes [3][Np][2 Sp] (zeros past N); part[block of rows][2 Sp]: sums over the block's rows, or null
 template <class T>
-__global__ __launch_bounds__(256) void gate_grad_kernel(const T* __restrict__ dH, const float* __restrict__ Z, int N, int S, int Sp,
-                                                        T* __restrict__ D, float* __restrict__ part) {
+__global__ __launch_bounds__(256) void gate_grad_kernel(const T* __restrict__ dH, const float* __restrict__ Z, int N, int Np, int S, int Sp,
+                                                        __bf16* __restrict__ D, float* __restrict__ part) {
+    constexpr bool planes = std::is_same<T, float>::value;
+    auto put = [&](__bf16* d, float (&x)[4]) __attribute__((always_inline)) {
+        if constexpr (planes) {
+            const size_t plane = (size_t)Np * 2 * Sp;
+            bf16x4 h, m, l;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                __bf16 a, b, c;
+                planes_of(x[i], a, b, c);
+                h[i] = a; m[i] = b; l[i] = c;
+            }
+            *reinterpret_cast<bf16x4*>(d) = h;
+            *reinterpret_cast<bf16x4*>(d + plane) = m;
+            *reinterpret_cast<bf16x4*>(d + 2 * plane) = l;
+        } else {
+            store4(d, x);
+        }
+    };
     __shared__ float red[4][2][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int s = blockIdx.x * 256 + 4 * lane;
-    const int n0 = blockIdx.y * GG_ROWS + wave * (GG_ROWS / 4), n1 = min(n0 + GG_ROWS / 4, N);
+    const int n0 = blockIdx.y * GG_ROWS + wave * (GG_ROWS / 4), n1 = min(n0 + GG_ROWS / 4, planes ? Np : N);
     float sg[4] = {}, su[4] = {};
     if (s < Sp) {
         for (int n = n0; n < n1; ++n) {
             const size_t e = (size_t)n * S + s;
             float h[4], p[4], q[4];
-            if (s + 4 <= S) {
+            if (s + 4 <= S && (!planes || n < N)) {
                 load4(dH + e, h);
                 load4(Z + e, p);
                 load4(Z + (size_t)N * S + e, q);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool in = s + i < S;
+                    const bool in = s + i < S && (!planes || n < N);
                     h[i] = in ? (float)dH[e + i] : 0.f;
                     p[i] = in ? Z[e + i] : 0.f;
                     q[i] = in ? Z[(size_t)N * S + e + i] : 0.f;
@@ -162,9 +300,9 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(const T* __restrict__ dH
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) { p[i] *= h[i]; q[i] *= h[i]; }
-            T* d = D + (size_t)n * 2 * Sp + s;
-            store4(d, p);
-            store4(d + Sp, q);
+            __bf16* d = D + (size_t)n * 2 * Sp + s;
+            put(d, p);
+            put(d + Sp, q);
 #pragma unroll
             for (int i = 0; i < 4; ++i) { sg[i] += p[i]; su[i] += q[i]; }
         }
@@ -220,24 +358,6 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const __bf16* __restrict_
     }
 }
 
-// out[c][col0 + r] = in[r][c] - mu[c], float32, row length `pitch`; rows r from R to Rp are written as zeros
-__global__ __launch_bounds__(256) void transpose_kernel(const float* __restrict__ in, int R, int C, int in_pitch, const float* __restrict__ mu,
-                                                        float* __restrict__ out, size_t pitch, int col0, int Rp) {
-    __shared__ float t[32][33];
-    const int r0 = blockIdx.x * 32, c0 = blockIdx.y * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
-#pragma unroll
-    for (int k = 0; k < 32; k += 8) {
-        const int r = r0 + y + k, c = c0 + x;
-        t[y + k][x] = r < R && c < C ? in[(size_t)r * in_pitch + c] - (mu ? mu[c] : 0.f) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 32; k += 8) {
-        const int c = c0 + y + k, r = r0 + x;
-        if (c < C && r < Rp) out[(size_t)c * pitch + col0 + r] = t[x][y + k];
-    }
-}
-
 inline unsigned blocks_for(size_t n) { return (unsigned)((n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384); }
 inline int up8(int m) { return (m + 7) / 8 * 8; }
 inline int up64(int s) { return (s + 63) / 64 * 64; }
@@ -251,8 +371,10 @@ fw_status pad_rows(const void* in, int R, int M, void* out, hipStream_t st) {
     FW_LAUNCH_CHECK();
     return FW_OK;
 }
-fw_status transpose(const float* in, int R, int C, int in_pitch, const float* mu, float* out, size_t pitch, int col0, int Rp, hipStream_t st) {
-    hipLaunchKernelGGL(transpose_kernel, dim3((Rp + 31) / 32, (C + 31) / 32), dim3(256), 0, st, in, R, C, in_pitch, mu, out, pitch, col0, Rp);
+fw_status split_planes(const Split& s, int matrices, int M, hipStream_t st) {
+    int rows = 0;
+    for (int k = 0; k < matrices; ++k) rows = s.Rp[k] > rows ? s.Rp[k] : rows;
+    hipLaunchKernelGGL(split_planes_kernel, dim3(blocks_for((size_t)rows * (up64(M) / 8)), matrices), dim3(256), 0, st, s, M, up64(M));
     FW_LAUNCH_CHECK();
     return FW_OK;
 }
@@ -268,84 +390,99 @@ struct Carve {
     }
 };
 
-// ---- the products' plans
-TileProduct forward_plan(int N, int M, int S) {
+// ---- the products' plans; float32 (planes): six passes over padded operands
+TileProduct forward_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = S; g.chunks = up8(M) / 8;
-    g.stages = g.part = (g.chunks + 7) / 8;
+    g.term = g.part = (g.chunks + 7) / 8;
+    g.stages = dt == FW_F32 ? 6 * g.term : g.term;
     tile_plan(g, true);
     return g;
 }
-TileProduct rows_plan(int N, int M, int S) {
+TileProduct rows_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = M; g.chunks = 2 * up64(S) / 8; g.klen = S;
-    g.part = up64(S) / 64; g.stages = 2 * g.part;
+    g.part = up64(S) / 64; g.term = 2 * g.part;
+    g.stages = dt == FW_F32 ? 6 * g.term : g.term;
     tile_plan(g, false);
     return g;
 }
-TileProduct weights_plan(int N, int M, int S) {
+TileProduct weights_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = 2 * up64(S); g.C = M; g.klen = N;
-    g.part = g.stages = (N + 63) / 64;
+    g.term = g.part = (N + 63) / 64;
+    g.stages = dt == FW_F32 ? 6 * g.term : g.term;
     tile_plan(g, false);
     return g;
 }
 
-struct ForwardWs { void *X, *Wg, *Wu, *partial; float* gu; size_t total; };
+size_t plane3_bytes(int R, int M) { return 6 * (size_t)R * up64(M); }
+struct ForwardWs { void *X, *Wg, *Wu, *partial; size_t total; };
 ForwardWs forward_ws(fw_dtype dt, int N, int M, int S, void* ws) {
     Carve c = {reinterpret_cast<char*>(ws)};
     ForwardWs w = {};
     if (dt == FW_F32) {
-        w.gu = reinterpret_cast<float*>(c.take(2 * (size_t)N * S * 4));
-    } else {
-        if (M % 8) {
-            w.X = c.take((size_t)N * up8(M) * 2);
-            w.Wg = c.take((size_t)S * up8(M) * 2);
-            w.Wu = c.take((size_t)S * up8(M) * 2);
+        if (N > FEW) {
+            w.X = c.take(plane3_bytes(N, M));
+            w.Wg = c.take(plane3_bytes(S, M));
+            w.Wu = c.take(plane3_bytes(S, M));
         }
-        w.partial = c.take(tile_partial_bytes(forward_plan(N, M, S)));
+    } else if (M % 8) {
+        w.X = c.take((size_t)N * up8(M) * 2);
+        w.Wg = c.take((size_t)S * up8(M) * 2);
+        w.Wu = c.take((size_t)S * up8(M) * 2);
     }
+    if (dt == FW_BF16 || N > FEW) w.partial = c.take(tile_partial_bytes(forward_plan(dt, N, M, S)));
     w.total = c.used;
     return w;
 }
-struct GradWs { void *D, *X, *Wg, *Wu, *partial; float *part, *sums, *Wt, *Dt, *Xt; size_t total; };
+struct GradWs { void *D, *X, *Wg, *Wu, *partial; float *part, *sums; size_t total; };
 GradWs grad_ws(fw_dtype dt, int N, int M, int S, void* ws) {
     Carve c = {reinterpret_cast<char*>(ws)};
     GradWs w = {};
     const size_t Sp = up64(S);
-    w.D = c.take((size_t)N * 2 * Sp * (dt == FW_BF16 ? 2 : 4));
+    w.D = c.take(dt == FW_F32 ? plane3_bytes(up64(N), 2 * (int)Sp) : (size_t)N * 2 * Sp * 2);
     w.part = reinterpret_cast<float*>(c.take((size_t)row_blocks(N) * 2 * Sp * 4));
     w.sums = reinterpret_cast<float*>(c.take(2 * Sp * 4));
     if (dt == FW_F32) {
-        w.Wt = reinterpret_cast<float*>(c.take((size_t)M * 2 * Sp * 4));
-        w.Dt = reinterpret_cast<float*>(c.take((size_t)N * 2 * Sp * 4));
-        w.Xt = reinterpret_cast<float*>(c.take((size_t)N * M * 4));
-    } else {
-        if (M % 8) {
-            w.X = c.take((size_t)N * up8(M) * 2);
-            w.Wg = c.take((size_t)S * up8(M) * 2);
-            w.Wu = c.take((size_t)S * up8(M) * 2);
-        }
-        const size_t a = tile_partial_bytes(rows_plan(N, M, S)), b = tile_partial_bytes(weights_plan(N, M, S));
-        w.partial = c.take(a > b ? a : b);
+        w.X = c.take(plane3_bytes(up64(N), M));
+        w.Wg = c.take(plane3_bytes((int)Sp, M));
+        w.Wu = c.take(plane3_bytes((int)Sp, M));
+    } else if (M % 8) {
+        w.X = c.take((size_t)N * up8(M) * 2);
+        w.Wg = c.take((size_t)S * up8(M) * 2);
+        w.Wu = c.take((size_t)S * up8(M) * 2);
     }
+    const size_t a = tile_partial_bytes(rows_plan(dt, N, M, S)), b = tile_partial_bytes(weights_plan(dt, N, M, S));
+    w.partial = c.take(a > b ? a : b);
     w.total = c.used;
     return w;
 }
 
 fw_status forward_f32(const float* X, int N, int M, int S, const float* Wg, const float* Wu, const float* bg, const float* bu, fw_act act,
                       float* H, float* Z, void* ws, hipStream_t st) {
-    const size_t n = (size_t)N * S;
-    float* gu = forward_ws(FW_F32, N, M, S, ws).gu;
-    for (int k = 0; k < 2; ++k) {
-        GemmEpilogue e = {};
-        e.out = gu + k * n; e.taps = 1;
-        const fw_status rc = gemm_planes(X, false, N, S, M, k ? Wu : Wg, e, false, st);
-        if (rc != FW_OK) return rc;
+    const ForwardWs w = forward_ws(FW_F32, N, M, S, ws);
+    const GateEpilogue<float> epi = {H, Z, bg, bu, N, S, (int)act, X, Wg, Wu, M};
+    if (N <= FEW) {
+        const auto launch = [&](auto NR) {
+            hipLaunchKernelGGL(few_rows_kernel<decltype(NR)::value>, dim3((S + 3) / 4, (N + decltype(NR)::value - 1) / decltype(NR)::value), dim3(256), 0, st,
+                               X, N, M, S, Wg, Wu, epi);
+        };
+        if (N == 1) launch(std::integral_constant<int, 1>());
+        else if (N <= 4) launch(std::integral_constant<int, 4>());
+        else launch(std::integral_constant<int, 8>());
+        FW_LAUNCH_CHECK();
+        return FW_OK;
     }
-    hipLaunchKernelGGL(gate_kernel, dim3(blocks_for(n)), dim3(256), 0, st, gu, n, S, bg, bu, (int)act, H, Z);
-    FW_LAUNCH_CHECK();
-    return FW_OK;
+    const Split s = {{X, Wg, Wu}, {(__bf16*)w.X, (__bf16*)w.Wg, (__bf16*)w.Wu}, {N, S, S}, {N, S, S}, {}};
+    const fw_status rc = split_planes(s, 3, M, st);
+    if (rc != FW_OK) return rc;
+    TileProduct g = forward_plan(FW_F32, N, M, S);
+    g.a = bytes(w.X); g.b0 = bytes(w.Wg); g.b1 = bytes(w.Wu);
+    g.apitch = g.bpitch = 2ll * up64(M);
+    g.aplane = N * g.apitch; g.bplane = S * g.bpitch;
+    g.partial = w.partial;
+    return tile_product<TILE_PLANES, false, false, true>(g, epi, st);
 }
 
 fw_status forward_bf16(const void* X, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu, fw_act act,
@@ -358,18 +495,18 @@ fw_status forward_bf16(const void* X, int N, int M, int S, const void* Wg, const
         if (rc != FW_OK) return rc;
         X = w.X; Wg = w.Wg; Wu = w.Wu;
     }
-    TileProduct g = forward_plan(N, M, S);
+    TileProduct g = forward_plan(FW_BF16, N, M, S);
     g.a = bytes(X); g.b0 = bytes(Wg); g.b1 = bytes(Wu);
     g.apitch = g.bpitch = 2ll * up8(M);
     g.partial = w.partial;
-    return tile_product<false, false, false, true>(g, GateEpilogue{reinterpret_cast<__bf16*>(H), Z, bg, bu, N, S, (int)act}, st);
+    return tile_product<TILE_BF16, false, false, true>(g, GateEpilogue<__bf16>{reinterpret_cast<__bf16*>(H), Z, bg, bu, N, S, (int)act}, st);
 }
 
 template <class T>
 fw_status gate_grad(const T* dH, const float* Z, int N, int S, const GradWs& w, bool sums, T* dbg, T* dbu, hipStream_t st) {
     const int Sp = up64(S);
-    hipLaunchKernelGGL(gate_grad_kernel<T>, dim3((Sp + 255) / 256, row_blocks(N)), dim3(256), 0, st, dH, Z, N, S, Sp, reinterpret_cast<T*>(w.D),
-                       sums ? w.part : nullptr);
+    hipLaunchKernelGGL(gate_grad_kernel<T>, dim3((Sp + 255) / 256, row_blocks(N)), dim3(256), 0, st, dH, Z, N, up64(N), S, Sp,
+                       reinterpret_cast<__bf16*>(w.D), sums ? w.part : nullptr);
     FW_LAUNCH_CHECK();
     if (!sums) return FW_OK;
     hipLaunchKernelGGL(bias_grad_kernel<T>, dim3((2 * Sp + 63) / 64), dim3(1024), 0, st, w.part, row_blocks(N), S, Sp, w.sums, dbg, dbu);
@@ -380,26 +517,33 @@ fw_status gate_grad(const T* dH, const float* Z, int N, int S, const GradWs& w, 
 fw_status grad_f32(const float* X, int N, int M, int S, const float* Wg, const float* Wu, const float* Z, const float* dH, const float* mu,
                    float* dX, float* dWg, float* dWu, float* dbg, float* dbu, void* ws, hipStream_t st) {
     const GradWs w = grad_ws(FW_F32, N, M, S, ws);
-    const int Sp = up64(S);
-    float* D = reinterpret_cast<float*>(w.D);
+    const int Sp = up64(S), Np = up64(N);
     fw_status rc = gate_grad<float>(dH, Z, N, S, w, dbg != nullptr, dbg, dbu, st);
     if (rc != FW_OK) return rc;
-    GemmEpilogue e = {};
-    e.taps = 1;
+    const GradInputs in = {X, Wg, Wu, Z, dH, mu, N, M, S};
+    Split s = {};
+    int k = 0;
+    const auto add = [&](const float* p, void* out, int R, int Rp, const float* c) { s.in[k] = p; s.out[k] = (__bf16*)out; s.R[k] = R; s.Rp[k] = Rp; s.mu[k++] = c; };
+    if (dWg) add(X, w.X, N, Np, mu);
+    if (dX) { add(Wg, w.Wg, S, Sp, nullptr); add(Wu, w.Wu, S, Sp, nullptr); }
+    if (k) rc = split_planes(s, k, M, st);
+    if (rc != FW_OK) return rc;
     if (dX) {
-        rc = transpose(Wg, S, M, M, nullptr, w.Wt, 2 * (size_t)Sp, 0, Sp, st);
-        if (rc == FW_OK) rc = transpose(Wu, S, M, M, nullptr, w.Wt, 2 * (size_t)Sp, Sp, Sp, st);
-        e.out = dX;
-        if (rc == FW_OK) rc = gemm_planes(D, false, N, M, 2 * Sp, w.Wt, e, false, st);
+        TileProduct g = rows_plan(FW_F32, N, M, S);
+        g.a = bytes(w.D); g.b0 = bytes(w.Wg); g.b1 = bytes(w.Wu);
+        g.apitch = 4ll * Sp; g.bpitch = 2ll * up64(M);
+        g.aplane = Np * g.apitch; g.bplane = Sp * g.bpitch;
+        g.partial = w.partial;
+        rc = tile_product<TILE_PLANES, false, true, false>(g, RowsEpilogue<float>{dX, N, M, in}, st);
         if (rc != FW_OK) return rc;
     }
     if (dWg) {
-        rc = transpose(X, N, M, M, mu, w.Xt, (size_t)N, 0, N, st);
-        if (rc == FW_OK) rc = transpose(D, N, 2 * Sp, 2 * Sp, nullptr, w.Dt, (size_t)N, 0, N, st);
-        for (int k = 0; k < 2 && rc == FW_OK; ++k) {
-            e.out = k ? dWu : dWg;
-            rc = gemm_planes(w.Dt + (size_t)k * Sp * N, false, S, M, N, w.Xt, e, false, st);
-        }
+        TileProduct g = weights_plan(FW_F32, N, M, S);
+        g.a = bytes(w.D); g.b0 = g.b1 = bytes(w.X);
+        g.apitch = 4ll * Sp; g.bpitch = 2ll * up64(M);
+        g.aplane = Np * g.apitch; g.bplane = Np * g.bpitch;
+        g.partial = w.partial;
+        rc = tile_product<TILE_PLANES, true, true, false>(g, WeightsEpilogue<float>{dWg, dWu, nullptr, nullptr, S, Sp, M, in}, st);
     }
     return rc;
 }
@@ -417,11 +561,11 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
         Wg = w.Wg; Wu = w.Wu;
     }
     if (dX) {
-        TileProduct g = rows_plan(N, M, S);
+        TileProduct g = rows_plan(FW_BF16, N, M, S);
         g.a = bytes(w.D); g.b0 = bytes(Wg); g.b1 = bytes(Wu);
         g.apitch = 4ll * Sp; g.bpitch = 2ll * up8(M);
         g.partial = w.partial;
-        rc = tile_product<false, false, true, false>(g, RowsEpilogue{dX, N, M}, st);
+        rc = tile_product<TILE_BF16, false, true, false>(g, RowsEpilogue<__bf16>{dX, N, M, {}}, st);
         if (rc != FW_OK) return rc;
     }
     if (dWg) {
@@ -430,11 +574,11 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
             if (rc != FW_OK) return rc;
             X = w.X;
         }
-        TileProduct g = weights_plan(N, M, S);
+        TileProduct g = weights_plan(FW_BF16, N, M, S);
         g.a = bytes(w.D); g.b0 = g.b1 = bytes(X);
         g.apitch = 4ll * Sp; g.bpitch = 2ll * up8(M);
         g.partial = w.partial;
-        rc = tile_product<false, true, true, false>(g, WeightsEpilogue{dWg, dWu, w.sums, mu, S, Sp, M}, st);
+        rc = tile_product<TILE_BF16, true, true, false>(g, WeightsEpilogue<__bf16>{dWg, dWu, w.sums, mu, S, Sp, M, {}}, st);
     }
     return rc;
 }

@@ -82,8 +82,8 @@ fw_status int8_product(const signed char* Xq, const float* sx, int N, int M, int
     g.apitch = g.bpitch = up16(M);
     g.partial = w ? w + padded_bytes(N, M) + padded_bytes(S, M) : nullptr;
     if (dt == FW_BF16)
-        return tile_product<true, false, false, false>(g, ScaleEpilogue<__bf16>{reinterpret_cast<__bf16*>(Y), sx, sw, b, N, S}, st);
-    return tile_product<true, false, false, false>(g, ScaleEpilogue<float>{reinterpret_cast<float*>(Y), sx, sw, b, N, S}, st);
+        return tile_product<TILE_I8, false, false, false>(g, ScaleEpilogue<__bf16>{reinterpret_cast<__bf16*>(Y), sx, sw, b, N, S}, st);
+    return tile_product<TILE_I8, false, false, false>(g, ScaleEpilogue<float>{reinterpret_cast<float*>(Y), sx, sw, b, N, S}, st);
 }
 
 }  // namespace fw

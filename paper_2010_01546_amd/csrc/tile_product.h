@@ -17,6 +17,11 @@
 //   Contraction-major (bfloat16; a row of memory is one k): a stage holds 64 k of all the panel's columns and is turned as it is read
 //     (ds_read_b64_tr_b16: 16 lanes get 4 k of a column each out of 4 x 16 entries).  Pairs of chunks, 16 columns, are permuted by a
 //     function of k that puts the eight k read together into different banks.  No transposed copy is made.
+// PLANES: float32 operands as three bfloat16 planes each, x = h + m + l (h = bf16(x), m = bf16(x - h), l = bf16(x - h - m), 24 bits; splitting
+//   into three: G. Henry, P. T. P. Tang, A. Heinecke 2019), aplane and bplane bytes apart.  The contraction goes by six times, over the
+//   pairs of planes above 2^-24 of the product, the small ones first: l h, h l, m m, m h, h m, h h, all into the same float32 sums.  The
+//   planes are padded with zeros to whole stages.  Entries below 2^-110 lose their last bits (bfloat16 ends at 2^-133); where a result is
+//   not finite (an infinite entry has no such sum) the epilogue computes it once more in float32.
 // Where the contraction ends inside a stage, the loads past the end fetch a zero (in both operands: 0 x NaN is NaN).  Rows or columns past
 // the edge are clamped; they feed results that the epilogue does not store.
 //
@@ -32,6 +37,8 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 
 static __device__ uint4 tile_zero;          // 16 bytes of zeros, never written
 
+enum TileKind { TILE_BF16, TILE_I8, TILE_PLANES };
+
 struct TileProduct {
     const char *a, *b0, *b1;      // operands; b1: a second matrix, of the same tile's other columns (PAIR) or of the contraction's second part
     long long apitch, bpitch;     // bytes between rows in memory
@@ -39,6 +46,8 @@ struct TileProduct {
     int chunks;                   // 16-byte chunks of a row (operands along the contraction)
     int klen;                     // k of a part (contraction-major operands)
     int part, stages;             // stages of the first part, stages in all
+    long long aplane, bplane;     // PLANES
+    int term;                     // PLANES: stages of one of the six passes
     int nrb, ncb, tiles, runs, spr;
     int nrt, nct;                 // tile shape
     void* partial;
@@ -78,6 +87,9 @@ template <int NRT, int NCT, int NW> struct TileShape {
     static constexpr int WR = 2 * NRT, WC = 4 * NCT / NWC;      // 16 x 16 results of a wavefront, down and across
     static constexpr int NT = 64 * NW;
     static constexpr int PA = 8192 * NRT, PB = 8192 * NCT;      // bytes of a stage of a panel
+    // stages of B in LDS, one more of A: what 160 KB hold
+    static constexpr int D = NRT + NCT >= 8 ? 2 : NRT + NCT >= 5 ? 3 : NRT + NCT == 4 ? 4 : 6;
+    static_assert((D + 1) * PA + D * PB <= 160 * 1024, "LDS of a compute unit");
 };
 template <int WC, bool PAIR> __device__ __forceinline__ int tile_column(int panel, int wj, int lane) {
     return panel + wj * (PAIR ? 8 * WC : 16 * WC) + 4 * (lane >> 4);
@@ -93,14 +105,15 @@ __device__ __forceinline__ void tile_apply(const Epi& epi, int n, int s, const A
 }
 
 // PAIR: the panel of B holds columns of b0 and the same columns of b1; results tb and tb + WC / 2 of a wavefront belong together.
-template <bool I8, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>
+template <TileKind KIND, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>
 __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g, Epi epi) {
     using Shape = TileShape<NRT, NCT, NW>;
-    constexpr int NWC = Shape::NWC, WR = Shape::WR, WC = Shape::WC;
+    constexpr bool I8 = KIND == TILE_I8, PLANES = KIND == TILE_PLANES;
+    constexpr int D = Shape::D, NWC = Shape::NWC, WR = Shape::WR, WC = Shape::WC;
     constexpr int LA = 8 * NRT / NW, LB = 8 * NCT / NW, NL = LA + LB;      // loads of a wavefront and stage
     constexpr int NF = WR + WC, NM = WR * WC;                             // fragments, matrix instructions
     using Acc = typename std::conditional<I8, intx4, floatx4>::type;
-    __shared__ __align__(1024) char lds[3 * Shape::PA + 2 * Shape::PB];     // three stages of A, two of B
+    __shared__ __align__(1024) char lds[(Shape::D + 1) * Shape::PA + Shape::D * Shape::PB];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / NWC, wj = wave % NWC;
@@ -160,10 +173,20 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     struct Stage { const char *a, *b; int c, cb; };
     auto stage_at = [&](int c) __attribute__((always_inline)) {
         Stage s;
+        s.c = c;
+        const char *a = base_a, *b = base_b;
+        if constexpr (PLANES) {
+            int term = 0;
+#pragma unroll
+            for (int t = 1; t < 6; ++t) term += c >= t * g.term ? 1 : 0;
+            c -= term * g.term;
+            a += (0x001102 >> (4 * term) & 15) * g.aplane;       // planes l h m m h h
+            b += (0x010120 >> (4 * term) & 15) * g.bplane;       // planes h l m h m h
+        }
         const bool two = BKM && c >= g.part;
-        s.c = c; s.cb = two ? c - g.part : c;
-        s.a = base_a + (AKM ? (long long)c * 64 * g.apitch : (long long)c * 128);
-        s.b = base_b + (BKM ? (long long)s.cb * 64 * g.bpitch + (two ? second : 0) : (long long)c * 128);
+        s.cb = two ? c - g.part : c;
+        s.a = a + (AKM ? (long long)c * 64 * g.apitch : (long long)c * 128);
+        s.b = b + (BKM ? (long long)s.cb * 64 * g.bpitch + (two ? second : 0) : (long long)c * 128);
         return s;
     };
     // ALL: the whole stage lies inside the contraction
@@ -175,7 +198,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
         } else {
             const int c = isa ? s.c : s.cb, RP = 8 / (isa ? NRT : NCT);
             const bool major = isa ? AKM : BKM;
-            const bool inside = s.c < cend && (major ? 64 * c + (wave + NW * (isa ? k : k - LA)) * RP + lane / (64 / RP) < g.klen
+            const bool inside = s.c < cend && (PLANES ? true : major ? 64 * c + (wave + NW * (isa ? k : k - LA)) * RP + lane / (64 / RP) < g.klen
                                                      : 8 * c + chunk < g.chunks);
             dma16(inside ? (const void*)((isa ? s.a : s.b) + vof[k]) : (const void*)&tile_zero, to);
         }
@@ -221,21 +244,21 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     };
 
     // At the barrier in the middle of stage c every wavefront holds the stage's second half in registers, so its buffers are free: in the
-    // half that follows the loads of B's stage c + 2 go out, in the half after that those of A's stage c + 3 (three buffers for A, two
-    // for B: what 160 KB hold for 256 x 256 results).  The loads of a wavefront complete in order; with those of A's stage c + 2
-    // outstanding all of stage c + 1 has landed for it, the barrier extends that to all.  Past the end the loads fetch zeros, which
-    // keeps their number the same.
+    // half that follows the loads of B's stage c + D go out, in the half after that those of A's stage c + D + 1.  The loads of a wavefront
+    // complete in order; with those behind B's stage c + 1 outstanding all of that stage has landed for it, the barrier extends that to
+    // all.  Past the end the loads fetch zeros, which keeps their number the same.  (Tiles with short stages need the depth: 1024 x 1152 x
+    // 9216 results of three planes each on 128 x 128 tiles, 0.7 us a stage with two stages in flight.)
     auto load_panel = [&](auto ISA, int to_buf, int c) __attribute__((always_inline)) {
         const Stage s = stage_at(c);
 #pragma unroll
         for (int k = decltype(ISA)::value ? 0 : LA; k < (decltype(ISA)::value ? LA : NL); ++k) load_one(std::false_type(), to_buf, s, k);
     };
-    constexpr int B0 = 3 * Shape::PA;
-    load_panel(std::true_type(), 0, c0);
-    load_panel(std::false_type(), B0, c0);
-    load_panel(std::true_type(), Shape::PA, c0 + 1);
-    load_panel(std::false_type(), B0 + Shape::PB, c0 + 1);
-    FW_WAIT_VM(NL);
+    constexpr int B0 = (D + 1) * Shape::PA, BE = B0 + D * Shape::PB;
+    for (int i = 0; i < D; ++i) {
+        load_panel(std::true_type(), i * Shape::PA, c0 + i);
+        load_panel(std::false_type(), B0 + i * Shape::PB, c0 + i);
+    }
+    FW_WAIT_VM((D - 1) * NL);
     __builtin_amdgcn_s_barrier();
     FW_COMPILER_FENCE();
 #pragma unroll
@@ -258,12 +281,12 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     int a0 = 0, b0 = B0;                         // the stage's buffers
     int c = c0;
     auto turn = [&](auto ALL) __attribute__((always_inline)) {
-        const int a1 = a0 == 2 * Shape::PA ? 0 : a0 + Shape::PA, a2 = a1 == 2 * Shape::PA ? 0 : a1 + Shape::PA;
-        const int b1 = 2 * B0 + Shape::PB - b0;
-        const Stage next = stage_at(c + 2);
-        half_turn(at_a + a0, at_b + b0, std::integral_constant<int, 0>(), std::true_type(), ALL, a2, next);
+        const int a1 = a0 == D * Shape::PA ? 0 : a0 + Shape::PA, free_a = a0 == 0 ? D * Shape::PA : a0 - Shape::PA;
+        const int b1 = b0 == BE - Shape::PB ? B0 : b0 + Shape::PB;
+        const Stage next = stage_at(c + D);
+        half_turn(at_a + a0, at_b + b0, std::integral_constant<int, 0>(), std::true_type(), ALL, free_a, next);
         FW_WAIT_LGKM0();
-        FW_WAIT_VM(LA);
+        FW_WAIT_VM((D - 1) * LA + (D - 2) * LB);
         __builtin_amdgcn_s_barrier();
         FW_COMPILER_FENCE();
         half_turn(at_a + a1, at_b + b1, std::integral_constant<int, 1>(), std::false_type(), ALL, b0, next);
@@ -272,7 +295,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     };
     while (c < cend) {
         // stages up to `fast` ask for whole ones only
-        const int fast = min(cend, BKM && c + 2 >= g.part ? g.part + whole : min(whole, g.part)) - 2;
+        const int fast = (PLANES ? cend : min(cend, BKM && c + D >= g.part ? g.part + whole : min(whole, g.part))) - D;
         while (c < fast) turn(std::true_type());
         turn(std::false_type());
     }
@@ -358,7 +381,7 @@ inline void tile_plan(TileProduct& g, bool pair) {
         const double t_mfma = 128.0 * nrt * nct + 60.0, t_load = (nrt + nct) * 8192.0 / 30.0, t_stage = t_mfma > t_load ? t_mfma : t_load;
         for (int runs = 1; runs <= 32 && (runs == 1 || (tiles * runs <= 512 && g.stages / runs >= 4)); ++runs) {
             const int spr = (g.stages + runs - 1) / runs, n = (g.stages + spr - 1) / spr;
-            double cost = (double)((tiles * n + 255) / 256) * (spr + 3.0) * t_stage;
+            double cost = (double)((tiles * n + 255) / 256) * (spr + 4.0) * t_stage;
             if (n > 1) cost += 6000.0 + 2.0 * n * tiles * (nrt * nct * 16384.0) / 4e12 * 2.1e9;
             if (cost < best * 0.999) {
                 best = cost;
@@ -371,26 +394,26 @@ inline size_t tile_partial_bytes(const TileProduct& g) {
     return g.runs > 1 ? align_up((size_t)g.runs * g.tiles * g.nrt * g.nct * 16384, 256) : 0;
 }
 
-template <bool I8, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>
+template <TileKind KIND, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>
 fw_status tile_launch(const TileProduct& g, const Epi& epi, hipStream_t st) {
     const long long total = (long long)g.tiles * g.runs;
     if (total > (1 << 30)) return FW_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((tile_product_kernel<I8, NRT, NCT, NW, AKM, BKM, PAIR, Epi>), dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * NW), 0, st, g, epi);
+    hipLaunchKernelGGL((tile_product_kernel<KIND, NRT, NCT, NW, AKM, BKM, PAIR, Epi>), dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * NW), 0, st, g, epi);
     FW_LAUNCH_CHECK();
     if (g.runs > 1) {
-        hipLaunchKernelGGL((tile_runs_kernel<I8, NRT, NCT, NW, PAIR, Epi>), dim3((unsigned)(g.tiles * 2 * NRT)), dim3(64 * NW), 0, st, g, epi);
+        hipLaunchKernelGGL((tile_runs_kernel<KIND == TILE_I8, NRT, NCT, NW, PAIR, Epi>), dim3((unsigned)(g.tiles * 2 * NRT)), dim3(64 * NW), 0, st, g, epi);
         FW_LAUNCH_CHECK();
     }
     return FW_OK;
 }
 
-template <bool I8, bool AKM, bool BKM, bool PAIR, class Epi>
+template <TileKind KIND, bool AKM, bool BKM, bool PAIR, class Epi>
 fw_status tile_product(const TileProduct& g, const Epi& epi, hipStream_t st) {
-    if (g.nrt == 4) return tile_launch<I8, 4, 4, 8, AKM, BKM, PAIR>(g, epi, st);
-    if (g.nrt == 2 && g.nct == 4) return tile_launch<I8, 2, 4, 8, AKM, BKM, PAIR>(g, epi, st);
-    if (g.nrt == 2) return tile_launch<I8, 2, 2, 8, AKM, BKM, PAIR>(g, epi, st);
-    if (g.nct == 4) return tile_launch<I8, 1, 4, 8, AKM, BKM, PAIR>(g, epi, st);
-    return tile_launch<I8, 1, 2, 8, AKM, BKM, PAIR>(g, epi, st);
+    if (g.nrt == 4) return tile_launch<KIND, 4, 4, 8, AKM, BKM, PAIR>(g, epi, st);
+    if (g.nrt == 2 && g.nct == 4) return tile_launch<KIND, 2, 4, 8, AKM, BKM, PAIR>(g, epi, st);
+    if (g.nrt == 2) return tile_launch<KIND, 2, 2, 8, AKM, BKM, PAIR>(g, epi, st);
+    if (g.nct == 4) return tile_launch<KIND, 1, 4, 8, AKM, BKM, PAIR>(g, epi, st);
+    return tile_launch<KIND, 1, 2, 8, AKM, BKM, PAIR>(g, epi, st);
 }
 
 }  // namespace fw
