@@ -427,7 +427,8 @@ fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, cons
  *   dWg, dWu    out  [S, M] element type `dt`, or both NULL
  *   dbg, dbu    out  [S] element type `dt`, or both NULL
  *   ws          scratch, fw_workspace_bytes(FW_OP_GATED_GRAD, M, S, d, dt) bytes
- * FW_BF16: dg and du are rounded to bfloat16 for the products, the sums are float32 and each result is rounded once.
+ * FW_BF16: dg and du are rounded to bfloat16 for the products (and for mu's part in them), the sums are float32 and each result is
+ * rounded once; dbg and dbu are sums of the values before that rounding.
  */
 fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* Z,
                         const void* dH, const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws,

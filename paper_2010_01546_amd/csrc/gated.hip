@@ -246,107 +246,114 @@ __device__ __forceinline__ void load4(const __bf16* p, float (&x)[4]) {
     for (int i = 0; i < 4; ++i) x[i] = (float)v[i];
 }
 __device__ __forceinline__ void load4(const float* p, float (&x)[4]) { __builtin_memcpy(x, p, 16); }
-__device__ __forceinline__ void store4(__bf16* p, float (&x)[4]) {     // x: as rounded
-    bf16x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[i] = (__bf16)x[i]; x[i] = (float)v[i]; }
-    __builtin_memcpy(p, &v, 8);
-}
-
-constexpr int GG_ROWS = 64;      // rows of a workgroup: 16 for each of its four wavefronts, 256 columns
-// D[n] = [dg | du] of row n, each Sp wide (zeros past S), float32 as three planes [3][Np][2 Sp] (zeros past N); part[block of rows][2 Sp]: sums over the block's rows, or null
+// D[n] = [dg | du] of row n, each Sp wide (zeros past S), float32 as three planes [3][Np][2 Sp] (zeros past N).  A workgroup has 256 columns
+// and `rows` rows, a wavefront a quarter of these, four at a time (their loads go out together).
+// part[block of rows][4][Sp] or null: sums over the block's rows of dg and du as they are (for the biases) and as rounded (for mu).
 template <class T>
 __global__ __launch_bounds__(256) void gate_grad_kernel(const T* __restrict__ dH, const float* __restrict__ Z, int N, int Np, int S, int Sp,
-                                                        __bf16* __restrict__ D, float* __restrict__ part) {
+                                                        int rows, __bf16* __restrict__ D, float* __restrict__ part) {
     constexpr bool planes = std::is_same<T, float>::value;
-    auto put = [&](__bf16* d, float (&x)[4]) __attribute__((always_inline)) {
-        if constexpr (planes) {
-            const size_t plane = (size_t)Np * 2 * Sp;
-            bf16x4 h, m, l;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                __bf16 a, b, c;
-                planes_of(x[i], a, b, c);
-                h[i] = a; m[i] = b; l[i] = c;
-            }
-            *reinterpret_cast<bf16x4*>(d) = h;
-            *reinterpret_cast<bf16x4*>(d + plane) = m;
-            *reinterpret_cast<bf16x4*>(d + 2 * plane) = l;
-        } else {
-            store4(d, x);
-        }
-    };
-    __shared__ float red[4][2][256];
+    __shared__ float red[4][4][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int s = blockIdx.x * 256 + 4 * lane;
-    const int n0 = blockIdx.y * GG_ROWS + wave * (GG_ROWS / 4), n1 = min(n0 + GG_ROWS / 4, planes ? Np : N);
-    float sg[4] = {}, su[4] = {};
-    if (s < Sp) {
-        for (int n = n0; n < n1; ++n) {
-            const size_t e = (size_t)n * S + s;
-            float h[4], p[4], q[4];
-            if (s + 4 <= S && (!planes || n < N)) {
-                load4(dH + e, h);
-                load4(Z + e, p);
-                load4(Z + (size_t)N * S + e, q);
+    const int n0 = blockIdx.y * rows + wave * (rows / 4), end = planes ? Np : N, n1 = min(n0 + rows / 4, end);
+    float sum[4][4] = {};
+    auto put = [&](__bf16* d, const float (&x)[4], float (&exact)[4], float (&rounded)[4]) __attribute__((always_inline)) {
+        bf16x4 h, m, l;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __bf16 a, b, c;
+            planes_of(x[i], a, b, c);
+            h[i] = a; m[i] = b; l[i] = c;
+            exact[i] += x[i];
+            rounded[i] += (float)a;
+        }
+        *reinterpret_cast<bf16x4*>(d) = h;
+        if (planes) {
+            const size_t plane = (size_t)Np * 2 * Sp;
+            *reinterpret_cast<bf16x4*>(d + plane) = m;
+            *reinterpret_cast<bf16x4*>(d + 2 * plane) = l;
+        }
+    };
+    auto rows_at = [&](auto WHOLE, int n) __attribute__((always_inline)) {       // WHOLE: four columns and four rows, all there
+        float h[4][4], p[4][4], q[4][4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const size_t e = (size_t)(n + r) * S + s;
+            if constexpr (decltype(WHOLE)::value) {
+                load4(dH + e, h[r]);
+                load4(Z + e, p[r]);
+                load4(Z + (size_t)N * S + e, q[r]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool in = s + i < S && (!planes || n < N);
-                    h[i] = in ? (float)dH[e + i] : 0.f;
-                    p[i] = in ? Z[e + i] : 0.f;
-                    q[i] = in ? Z[(size_t)N * S + e + i] : 0.f;
+                    const bool in = n + r < N && s + i < S;
+                    h[r][i] = in ? (float)dH[e + i] : 0.f;
+                    p[r][i] = in ? Z[e + i] : 0.f;
+                    q[r][i] = in ? Z[(size_t)N * S + e + i] : 0.f;
                 }
             }
+        }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { p[i] *= h[i]; q[i] *= h[i]; }
-            __bf16* d = D + (size_t)n * 2 * Sp + s;
-            put(d, p);
-            put(d + Sp, q);
+        for (int r = 0; r < 4; ++r) {
+            if (!decltype(WHOLE)::value && n + r >= n1) break;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { sg[i] += p[i]; su[i] += q[i]; }
+            for (int i = 0; i < 4; ++i) { p[r][i] *= h[r][i]; q[r][i] *= h[r][i]; }
+            __bf16* d = D + (size_t)(n + r) * 2 * Sp + s;
+            put(d, p[r], sum[0], sum[2]);
+            put(d + Sp, q[r], sum[1], sum[3]);
+        }
+    };
+    if (s < Sp) {
+        for (int n = n0; n < n1; n += 4) {
+            if (s + 4 <= S && n + 4 <= min(n1, N)) rows_at(std::true_type(), n);
+            else rows_at(std::false_type(), n);
         }
     }
     if (!part) return;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { red[wave][0][4 * lane + i] = sg[i]; red[wave][1][4 * lane + i] = su[i]; }
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red[wave][k][4 * lane + i] = sum[k][i];
     __syncthreads();
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c < Sp) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            part[((size_t)blockIdx.y * 2 + k) * Sp + c] =
+        for (int k = 0; k < 4; ++k)
+            part[((size_t)blockIdx.y * 4 + k) * Sp + c] =
                 red[0][k][threadIdx.x] + red[1][k][threadIdx.x] + red[2][k][threadIdx.x] + red[3][k][threadIdx.x];
     }
 }
 
-// sums[c] = the blocks' partial sums, in a fixed order; the biases' gradients where they are asked for
+// sums[c] = the blocks' partial sums, in a fixed order: of dg and du for the biases' gradients, of their rounded values for mu
 template <class T>
 __global__ __launch_bounds__(1024) void bias_grad_kernel(const float* __restrict__ part, int blocks, int S, int Sp, float* __restrict__ sums,
                                                          T* __restrict__ dbg, T* __restrict__ dbu) {
     __shared__ float red[16][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;    // Sp is a multiple of 64
+    const bool rounded = c >= 2 * Sp;
+    if (!rounded && !dbg) return;                                                   // the whole workgroup
     float v = 0.f;
-    if (c < 2 * Sp)
-        for (int p = slice; p < blocks; p += 16) v += part[(size_t)p * 2 * Sp + c];
+    for (int p = slice; p < blocks; p += 16) v += part[(size_t)p * 4 * Sp + c];
     red[slice][threadIdx.x & 63] = v;
     __syncthreads();
-    if (slice || c >= 2 * Sp) return;
+    if (slice) return;
     v = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) v += red[i][threadIdx.x];
-    sums[c] = v;
-    const int s = c >= Sp ? c - Sp : c;
-    if (dbg && s < S) (c >= Sp ? dbu : dbg)[s] = (T)v;
+    if (rounded) sums[c - 2 * Sp] = v;
+    else if (c % Sp < S) (c >= Sp ? dbu : dbg)[c % Sp] = (T)v;
 }
 
-// rows of M bfloat16 numbers to rows of Mp (a multiple of 8), zeros behind
-__global__ __launch_bounds__(256) void pad_rows_kernel(const __bf16* __restrict__ in, int M, int Mp, size_t n8, bf16x8* __restrict__ out) {
-    const int c8 = Mp / 8;
+// matrices of M bfloat16 columns to rows of Mp (a multiple of 8), zeros behind; the matrix goes by blockIdx.y
+struct Pad { const __bf16* in[3]; bf16x8* out[3]; int R[3]; };
+__global__ __launch_bounds__(256) void pad_rows_kernel(Pad s, int M, int Mp) {
+    const int k = blockIdx.y, c8 = Mp / 8;
+    const size_t n8 = (size_t)s.R[k] * c8;
     for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < n8; e += (size_t)gridDim.x * 256) {
         const size_t r = e / c8;
         const int m = 8 * (int)(e - r * c8);
-        const __bf16* p = in + r * M + m;
+        const __bf16* p = s.in[k] + r * M + m;
         bf16x8 v;
         if (m + 8 <= M) {
             __builtin_memcpy(&v, p, 16);
@@ -354,23 +361,34 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const __bf16* __restrict_
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = m + i < M ? p[i] : (__bf16)0.f;
         }
-        out[e] = v;
+        s.out[k][e] = v;
     }
 }
 
 inline unsigned blocks_for(size_t n) { return (unsigned)((n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384); }
 inline int up8(int m) { return (m + 7) / 8 * 8; }
 inline int up64(int s) { return (s + 63) / 64 * 64; }
-inline int row_blocks(int N) { return (N + GG_ROWS - 1) / GG_ROWS; }
+// rows of a workgroup of gate_grad_kernel: 64, or 16 where that leaves compute units without work (777 x 1001: 13.9 us with 64)
+inline int grad_rows(int N, int S) { return (long long)((N + 63) / 64) * ((S + 255) / 256) >= 1024 ? 64 : 16; }
+inline int row_blocks(int N, int S) { return (up64(N) + grad_rows(N, S) - 1) / grad_rows(N, S); }
 inline const char* bytes(const void* p) { return reinterpret_cast<const char*>(p); }
 
-fw_status pad_rows(const void* in, int R, int M, void* out, hipStream_t st) {
-    const size_t n8 = (size_t)R * (up8(M) / 8);
-    hipLaunchKernelGGL(pad_rows_kernel, dim3(blocks_for(n8)), dim3(256), 0, st, reinterpret_cast<const __bf16*>(in), M, up8(M), n8,
-                       reinterpret_cast<bf16x8*>(out));
-    FW_LAUNCH_CHECK();
-    return FW_OK;
-}
+struct PadList {
+    Pad s = {};
+    int n = 0, rows = 0;
+    void add(const void* in, int R, void* out) {
+        s.in[n] = reinterpret_cast<const __bf16*>(in);
+        s.out[n] = reinterpret_cast<bf16x8*>(out);
+        s.R[n++] = R;
+        rows = R > rows ? R : rows;
+    }
+    fw_status launch(int M, hipStream_t st) const {
+        if (!n) return FW_OK;
+        hipLaunchKernelGGL(pad_rows_kernel, dim3(blocks_for((size_t)rows * (up8(M) / 8)), n), dim3(256), 0, st, s, M, up8(M));
+        FW_LAUNCH_CHECK();
+        return FW_OK;
+    }
+};
 fw_status split_planes(const Split& s, int matrices, int M, hipStream_t st) {
     int rows = 0;
     for (int k = 0; k < matrices; ++k) rows = s.Rp[k] > rows ? s.Rp[k] : rows;
@@ -442,7 +460,7 @@ GradWs grad_ws(fw_dtype dt, int N, int M, int S, void* ws) {
     GradWs w = {};
     const size_t Sp = up64(S);
     w.D = c.take(dt == FW_F32 ? plane3_bytes(up64(N), 2 * (int)Sp) : (size_t)N * 2 * Sp * 2);
-    w.part = reinterpret_cast<float*>(c.take((size_t)row_blocks(N) * 2 * Sp * 4));
+    w.part = reinterpret_cast<float*>(c.take((size_t)row_blocks(N, S) * 4 * Sp * 4));
     w.sums = reinterpret_cast<float*>(c.take(2 * Sp * 4));
     if (dt == FW_F32) {
         w.X = c.take(plane3_bytes(up64(N), M));
@@ -489,9 +507,11 @@ fw_status forward_bf16(const void* X, int N, int M, int S, const void* Wg, const
                        void* H, float* Z, void* ws, hipStream_t st) {
     const ForwardWs w = forward_ws(FW_BF16, N, M, S, ws);
     if (M % 8) {             // 16-byte loads need aligned rows
-        fw_status rc = pad_rows(X, N, M, w.X, st);
-        if (rc == FW_OK) rc = pad_rows(Wg, S, M, w.Wg, st);
-        if (rc == FW_OK) rc = pad_rows(Wu, S, M, w.Wu, st);
+        PadList pads;
+        pads.add(X, N, w.X);
+        pads.add(Wg, S, w.Wg);
+        pads.add(Wu, S, w.Wu);
+        const fw_status rc = pads.launch(M, st);
         if (rc != FW_OK) return rc;
         X = w.X; Wg = w.Wg; Wu = w.Wu;
     }
@@ -505,11 +525,11 @@ fw_status forward_bf16(const void* X, int N, int M, int S, const void* Wg, const
 template <class T>
 fw_status gate_grad(const T* dH, const float* Z, int N, int S, const GradWs& w, bool sums, T* dbg, T* dbu, hipStream_t st) {
     const int Sp = up64(S);
-    hipLaunchKernelGGL(gate_grad_kernel<T>, dim3((Sp + 255) / 256, row_blocks(N)), dim3(256), 0, st, dH, Z, N, up64(N), S, Sp,
-                       reinterpret_cast<__bf16*>(w.D), sums ? w.part : nullptr);
+    hipLaunchKernelGGL(gate_grad_kernel<T>, dim3((Sp + 255) / 256, row_blocks(N, S)), dim3(256), 0, st, dH, Z, N, up64(N), S, Sp,
+                       grad_rows(N, S), reinterpret_cast<__bf16*>(w.D), sums ? w.part : nullptr);
     FW_LAUNCH_CHECK();
     if (!sums) return FW_OK;
-    hipLaunchKernelGGL(bias_grad_kernel<T>, dim3((2 * Sp + 63) / 64), dim3(1024), 0, st, w.part, row_blocks(N), S, Sp, w.sums, dbg, dbu);
+    hipLaunchKernelGGL(bias_grad_kernel<T>, dim3(4 * Sp / 64), dim3(1024), 0, st, w.part, row_blocks(N, S), S, Sp, w.sums, dbg, dbu);
     FW_LAUNCH_CHECK();
     return FW_OK;
 }
@@ -554,11 +574,13 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
     const int Sp = up64(S);
     fw_status rc = gate_grad<__bf16>(dH, Z, N, S, w, dbg || (mu && dWg), dbg, dbu, st);
     if (rc != FW_OK) return rc;
-    if (M % 8 && dX) {
-        rc = pad_rows(Wg, S, M, w.Wg, st);
-        if (rc == FW_OK) rc = pad_rows(Wu, S, M, w.Wu, st);
+    if (M % 8) {
+        PadList pads;
+        if (dX) { pads.add(Wg, S, w.Wg); pads.add(Wu, S, w.Wu); }
+        if (dWg) pads.add(X, N, w.X);
+        rc = pads.launch(M, st);
         if (rc != FW_OK) return rc;
-        Wg = w.Wg; Wu = w.Wu;
+        X = w.X; Wg = w.Wg; Wu = w.Wu;
     }
     if (dX) {
         TileProduct g = rows_plan(FW_BF16, N, M, S);
@@ -569,11 +591,6 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
         if (rc != FW_OK) return rc;
     }
     if (dWg) {
-        if (M % 8) {
-            rc = pad_rows(X, N, M, w.X, st);
-            if (rc != FW_OK) return rc;
-            X = w.X;
-        }
         TileProduct g = weights_plan(FW_BF16, N, M, S);
         g.a = bytes(w.D); g.b0 = g.b1 = bytes(X);
         g.apitch = 4ll * Sp; g.bpitch = 2ll * up8(M);

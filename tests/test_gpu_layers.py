@@ -271,8 +271,9 @@ def test_gated_gradient(N, M, S, dtype):
     within(dX.host(), want[0], ((2 * S + 8) * U32 + more) * (ag @ np.abs(lo.f64(Wg)) + au @ np.abs(lo.f64(Wu))) + half * np.abs(want[0]), "dX")
     within(dWg.host(), want[1], ((2 * N + 8) * U32 + more) * (ag.T @ aX) + half * np.abs(want[1]), "dWg")
     within(dWu.host(), want[2], ((2 * N + 8) * U32 + more) * (au.T @ aX) + half * np.abs(want[2]), "dWu")
-    within(dbg.host(), want[3], ((N + 4) * U32 + more) * ag.sum(0) + half * np.abs(want[3]), "dbg")
-    within(dbu.host(), want[4], ((N + 4) * U32 + more) * au.sum(0) + half * np.abs(want[4]), "dbu")
+    for got, factor, what in ((dbg, Zh[0], "dbg"), (dbu, Zh[1], "dbu")):      # of the products before their rounding to the type
+        d = lo.f64(dH) * factor
+        within(got.host(), d.sum(0), (N + 5) * U32 * np.abs(d).sum(0) + half * np.abs(d.sum(0)), what)
     # against the whole formula in 64 bits: dg and du and the results have a rounding each, of at most `half`; float32 adds its sums
     full = lo.gated_grad(X, Wg, Wu, kind, dH, bg, bu, mu)
     if kind != "relu":
