@@ -25,8 +25,9 @@
 // Where the contraction ends inside a stage, the loads past the end fetch a zero (in both operands: 0 x NaN is NaN).  Rows or columns past
 // the edge are clamped; they feed results that the epilogue does not store.
 //
-// Few tiles: the contraction is cut into runs over more workgroups; these leave their sums in a workspace, in the order of the accumulation
-// registers, and a second launch adds them in order and applies the epilogue.
+// Tiles that do not fill the chip (few tiles, or the rest behind whole rounds of 256): the contraction of these is cut into runs over more
+// workgroups, which leave their sums in a workspace, in the order of the accumulation registers; a second launch adds them in order and
+// applies the epilogue.
 #include "fw_internal.h"
 #include <type_traits>
 
@@ -48,7 +49,9 @@ struct TileProduct {
     int part, stages;             // stages of the first part, stages in all
     long long aplane, bplane;     // PLANES
     int term;                     // PLANES: stages of one of the six passes
-    int nrb, ncb, tiles, runs, spr;
+    int nrb, ncb;                 // rows and columns of tiles
+    int full, rest;               // tiles with the whole contraction, tiles cut into runs (none where runs is 1)
+    int runs, spr;                // runs, stages of a run
     int nrt, nct;                 // tile shape
     void* partial;
 };
@@ -117,16 +120,25 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / NWC, wj = wave % NWC;
-    // workgroups go to the 8 XCDs in turn: each XCD gets a contiguous run of tiles
-    const int total = g.tiles * g.runs, per_xcd = (total + 7) / 8;
-    int tile = ((int)blockIdx.x & 7) * per_xcd + ((int)blockIdx.x >> 3);
-    if (tile >= total || ((int)blockIdx.x >> 3) >= per_xcd) return;
-    const int run = __builtin_amdgcn_readfirstlane(tile / g.tiles);
-    tile -= run * g.tiles;
+    // workgroups go to the 8 XCDs in turn: each XCD gets a contiguous piece of the whole tiles, then one of the runs
+    const int items = g.rest * g.runs, per_full = (g.full + 7) / 8, per_run = (items + 7) / 8;
+    int at = (int)blockIdx.x >> 3;
+    int tile, run = 0, c0 = 0, cend = g.stages;
+    const bool cut = at >= per_full;
+    if (cut) {
+        at += ((int)blockIdx.x & 7) * per_run - per_full;
+        if (at >= items) return;
+        run = __builtin_amdgcn_readfirstlane(at / g.rest);
+        tile = g.full + at - run * g.rest;
+        c0 = run * g.spr;
+        cend = min(c0 + g.spr, g.stages);
+    } else {
+        tile = ((int)blockIdx.x & 7) * per_full + at;
+        if (tile >= g.full) return;
+    }
     int I, J;
     tile_at(g, tile, I, J);
     I = __builtin_amdgcn_readfirstlane(I); J = __builtin_amdgcn_readfirstlane(J);
-    const int c0 = run * g.spr, cend = min(c0 + g.spr, g.stages);
 
     // What this lane brings: of each panel a wavefront loads 1 KB pieces wave, wave + NW, ..., from base_a or base_b (the same for the
     // wavefront) + the stage's offset + vof[k]
@@ -302,8 +314,8 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     FW_WAIT_VM(0);
     FW_WAIT_LGKM0();
 
-    if (g.runs > 1) {
-        Acc* out = reinterpret_cast<Acc*>(g.partial) + ((size_t)run * g.tiles + tile) * (NM * Shape::NT) + tid;
+    if (cut) {
+        Acc* out = reinterpret_cast<Acc*>(g.partial) + ((size_t)run * g.rest + tile - g.full) * (NM * Shape::NT) + tid;
 #pragma unroll
         for (int ta = 0; ta < WR; ++ta)
 #pragma unroll
@@ -324,13 +336,13 @@ __global__ __launch_bounds__(64 * NW) void tile_runs_kernel(TileProduct g, Epi e
     const int tile = blockIdx.x / WR, ta = blockIdx.x % WR;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = wave / Shape::NWC, wj = wave % Shape::NWC;
     int I, J;
-    tile_at(g, tile, I, J);
+    tile_at(g, g.full + tile, I, J);
     Acc acc[WC];
     const Acc* in = reinterpret_cast<const Acc*>(g.partial) + ((size_t)tile * WR + ta) * (WC * Shape::NT) + tid;
 #pragma unroll
     for (int tb = 0; tb < WC; ++tb) acc[tb] = in[tb * Shape::NT];
     for (int z = 1; z < g.runs; ++z) {
-        in += (size_t)g.tiles * (WR * WC * Shape::NT);
+        in += (size_t)g.rest * (WR * WC * Shape::NT);
 #pragma unroll
         for (int tb = 0; tb < WC; ++tb) {
             const Acc v = in[tb * Shape::NT];
@@ -368,9 +380,9 @@ __device__ __forceinline__ void tile_vector(const float* p, int s, int cols, flo
     for (int i = 0; i < 4; ++i) v[i] = p && s + i < cols ? p[s + i] : 0.f;
 }
 
-// Tile shape and runs of the least estimated time in cycles: rounds of 256 workgroups x (stages of a run + filling the ring) x the longer
-// of a stage's matrix instructions and its loads (about 30 bytes per cycle and compute unit), plus the pass that adds the runs.  A run
-// keeps at least 4 stages.
+// Tile shape and runs of the least estimated time in cycles: rounds of 256 workgroups x (stages + filling the ring) x the longer of a stage's
+// matrix instructions and its loads (about 30 bytes per cycle and compute unit), plus the pass that adds the runs.  Runs are for the tiles
+// behind whole rounds, and keep at least 4 stages.
 inline void tile_plan(TileProduct& g, bool pair) {
     static const int shapes[][2] = {{4, 4}, {2, 4}, {2, 2}, {1, 4}, {1, 2}};
     double best = 1e300;
@@ -379,29 +391,29 @@ inline void tile_plan(TileProduct& g, bool pair) {
         const int nrb = (g.R + 64 * nrt - 1) / (64 * nrt), ncb = (g.C + tc - 1) / tc;
         const long long tiles = (long long)nrb * ncb;
         const double t_mfma = 128.0 * nrt * nct + 60.0, t_load = (nrt + nct) * 8192.0 / 30.0, t_stage = t_mfma > t_load ? t_mfma : t_load;
-        for (int runs = 1; runs <= 32 && (runs == 1 || (tiles * runs <= 512 && g.stages / runs >= 4)); ++runs) {
+        const int rest = (int)(tiles % 256);
+        for (int runs = 1; runs <= 32 && (runs == 1 || (rest > 0 && rest * runs <= 512 && g.stages / runs >= 4)); ++runs) {
             const int spr = (g.stages + runs - 1) / runs, n = (g.stages + spr - 1) / spr;
-            double cost = (double)((tiles * n + 255) / 256) * (spr + 4.0) * t_stage;
-            if (n > 1) cost += 6000.0 + 2.0 * n * tiles * (nrt * nct * 16384.0) / 4e12 * 2.1e9;
+            double cost = (double)((n > 1 ? tiles : tiles + 255) / 256) * (g.stages + 4.0) * t_stage;
+            if (n > 1) cost += (double)((rest * n + 255) / 256) * (spr + 4.0) * t_stage + 6000.0 + 2.0 * n * rest * (nrt * nct * 16384.0) / 4e12 * 2.1e9;
             if (cost < best * 0.999) {
                 best = cost;
-                g.nrt = nrt; g.nct = nct; g.nrb = nrb; g.ncb = ncb; g.tiles = (int)tiles; g.runs = n; g.spr = spr;
+                g.nrt = nrt; g.nct = nct; g.nrb = nrb; g.ncb = ncb; g.runs = n; g.spr = spr;
+                g.rest = n > 1 ? rest : 0; g.full = (int)tiles - g.rest;
             }
         }
     }
 }
-inline size_t tile_partial_bytes(const TileProduct& g) {
-    return g.runs > 1 ? align_up((size_t)g.runs * g.tiles * g.nrt * g.nct * 16384, 256) : 0;
-}
+inline size_t tile_partial_bytes(const TileProduct& g) { return align_up((size_t)g.rest * g.runs * g.nrt * g.nct * 16384, 256); }
 
 template <TileKind KIND, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>
 fw_status tile_launch(const TileProduct& g, const Epi& epi, hipStream_t st) {
-    const long long total = (long long)g.tiles * g.runs;
-    if (total > (1 << 30)) return FW_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((tile_product_kernel<KIND, NRT, NCT, NW, AKM, BKM, PAIR, Epi>), dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * NW), 0, st, g, epi);
+    if ((long long)g.nrb * g.ncb > (1 << 28)) return FW_ERR_UNSUPPORTED;
+    const unsigned groups = 8u * (unsigned)((g.full + 7) / 8 + (g.rest * g.runs + 7) / 8);
+    hipLaunchKernelGGL((tile_product_kernel<KIND, NRT, NCT, NW, AKM, BKM, PAIR, Epi>), dim3(groups), dim3(64 * NW), 0, st, g, epi);
     FW_LAUNCH_CHECK();
-    if (g.runs > 1) {
-        hipLaunchKernelGGL((tile_runs_kernel<KIND == TILE_I8, NRT, NCT, NW, PAIR, Epi>), dim3((unsigned)(g.tiles * 2 * NRT)), dim3(64 * NW), 0, st, g, epi);
+    if (g.rest) {
+        hipLaunchKernelGGL((tile_runs_kernel<KIND == TILE_I8, NRT, NCT, NW, PAIR, Epi>), dim3((unsigned)(g.rest * 2 * NRT)), dim3(64 * NW), 0, st, g, epi);
         FW_LAUNCH_CHECK();
     }
     return FW_OK;
