@@ -408,29 +408,26 @@ struct Carve {
     }
 };
 
-// ---- the products' plans; float32 (planes): six passes over padded operands
+// ---- the products' plans; float32 (planes): over padded operands
 TileProduct forward_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = S; g.chunks = up8(M) / 8;
-    g.term = g.part = (g.chunks + 7) / 8;
-    g.stages = dt == FW_F32 ? 6 * g.term : g.term;
-    tile_plan(g, true);
+    g.stages = g.part = (g.chunks + 7) / 8;
+    tile_plan(g, true, dt == FW_F32);
     return g;
 }
 TileProduct rows_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = M; g.chunks = 2 * up64(S) / 8; g.klen = S;
-    g.part = up64(S) / 64; g.term = 2 * g.part;
-    g.stages = dt == FW_F32 ? 6 * g.term : g.term;
-    tile_plan(g, false);
+    g.part = up64(S) / 64; g.stages = 2 * g.part;
+    tile_plan(g, false, dt == FW_F32);
     return g;
 }
 TileProduct weights_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = 2 * up64(S); g.C = M; g.klen = N;
-    g.term = g.part = (N + 63) / 64;
-    g.stages = dt == FW_F32 ? 6 * g.term : g.term;
-    tile_plan(g, false);
+    g.part = g.stages = (N + 63) / 64;
+    tile_plan(g, false, dt == FW_F32);
     return g;
 }
 

@@ -17,11 +17,12 @@
 //   Contraction-major (bfloat16; a row of memory is one k): a stage holds 64 k of all the panel's columns and is turned as it is read
 //     (ds_read_b64_tr_b16: 16 lanes get 4 k of a column each out of 4 x 16 entries).  Pairs of chunks, 16 columns, are permuted by a
 //     function of k that puts the eight k read together into different banks.  No transposed copy is made.
-// PLANES: float32 operands as three bfloat16 planes each, x = h + m + l (h = bf16(x), m = bf16(x - h), l = bf16(x - h - m), 24 bits; splitting
-//   into three: G. Henry, P. T. P. Tang, A. Heinecke 2019), aplane and bplane bytes apart.  The contraction goes by six times, over the
-//   pairs of planes above 2^-24 of the product, the small ones first: l h, h l, m m, m h, h m, h h, all into the same float32 sums.  The
-//   planes are padded with zeros to whole stages.  Entries below 2^-110 lose their last bits (bfloat16 ends at 2^-133); where a result is
-//   not finite (an infinite entry has no such sum) the epilogue computes it once more in float32.
+// TILE_PLANES: float32 operands as three bfloat16 planes each, x = h + m + l (h = bf16(x), m = bf16(x - h), l = bf16(x - h - m), 24 bits;
+//   splitting into three: G. Henry, P. T. P. Tang, A. Heinecke 2019), aplane and bplane bytes apart.  A stage holds all planes of both
+//   panels; of their nine products the six above 2^-24 go into the same float32 sums: l h, m h, h h, h m, m m, h l.  (Every pair of planes
+//   as a product of its own, each with its loads: 1024 x 576 x 2304, 61 us forward; loads bound it.)  The planes are padded with zeros to
+//   whole stages.  Entries below 2^-110 lose their last bits (bfloat16 ends at 2^-133); where a result is not finite (an infinite entry
+//   has no such sum) the epilogue computes it once more in float32.
 // Where the contraction ends inside a stage, the loads past the end fetch a zero (in both operands: 0 x NaN is NaN).  Rows or columns past
 // the edge are clamped; they feed results that the epilogue does not store.
 //
@@ -47,8 +48,7 @@ struct TileProduct {
     int chunks;                   // 16-byte chunks of a row (operands along the contraction)
     int klen;                     // k of a part (contraction-major operands)
     int part, stages;             // stages of the first part, stages in all
-    long long aplane, bplane;     // PLANES
-    int term;                     // PLANES: stages of one of the six passes
+    long long aplane, bplane;     // TILE_PLANES: bytes between planes
     int nrb, ncb;                 // rows and columns of tiles
     int full, rest;               // tiles with the whole contraction, tiles cut into runs (none where runs is 1)
     int runs, spr;                // runs, stages of a run
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     constexpr int LA = 8 * NRT / NW, LB = 8 * NCT / NW, NL = LA + LB;      // loads of a wavefront and stage
     constexpr int NF = WR + WC, NM = WR * WC;                             // fragments, matrix instructions
     using Acc = typename std::conditional<I8, intx4, floatx4>::type;
-    __shared__ __align__(1024) char lds[(Shape::D + 1) * Shape::PA + Shape::D * Shape::PB];
+    __shared__ __align__(1024) char lds[PLANES ? 3 * (Shape::PA + Shape::PB) : (D + 1) * Shape::PA + D * Shape::PB];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / NWC, wj = wave % NWC;
@@ -186,19 +186,10 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     auto stage_at = [&](int c) __attribute__((always_inline)) {
         Stage s;
         s.c = c;
-        const char *a = base_a, *b = base_b;
-        if constexpr (PLANES) {
-            int term = 0;
-#pragma unroll
-            for (int t = 1; t < 6; ++t) term += c >= t * g.term ? 1 : 0;
-            c -= term * g.term;
-            a += (0x001102 >> (4 * term) & 15) * g.aplane;       // planes l h m m h h
-            b += (0x010120 >> (4 * term) & 15) * g.bplane;       // planes h l m h m h
-        }
         const bool two = BKM && c >= g.part;
         s.cb = two ? c - g.part : c;
-        s.a = a + (AKM ? (long long)c * 64 * g.apitch : (long long)c * 128);
-        s.b = b + (BKM ? (long long)s.cb * 64 * g.bpitch + (two ? second : 0) : (long long)c * 128);
+        s.a = base_a + (AKM ? (long long)c * 64 * g.apitch : (long long)c * 128);
+        s.b = base_b + (BKM ? (long long)s.cb * 64 * g.bpitch + (two ? second : 0) : (long long)c * 128);
         return s;
     };
     // ALL: the whole stage lies inside the contraction
@@ -210,7 +201,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
         } else {
             const int c = isa ? s.c : s.cb, RP = 8 / (isa ? NRT : NCT);
             const bool major = isa ? AKM : BKM;
-            const bool inside = s.c < cend && (PLANES ? true : major ? 64 * c + (wave + NW * (isa ? k : k - LA)) * RP + lane / (64 / RP) < g.klen
+            const bool inside = s.c < cend && (major ? 64 * c + (wave + NW * (isa ? k : k - LA)) * RP + lane / (64 / RP) < g.klen
                                                      : 8 * c + chunk < g.chunks);
             dma16(inside ? (const void*)((isa ? s.a : s.b) + vof[k]) : (const void*)&tile_zero, to);
         }
@@ -255,29 +246,11 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
                                                                   __builtin_bit_cast(bf16x8, fr[half][ta]), acc[ta][tb], 0, 0, 0);
     };
 
-    // At the barrier in the middle of stage c every wavefront holds the stage's second half in registers, so its buffers are free: in the
-    // half that follows the loads of B's stage c + D go out, in the half after that those of A's stage c + D + 1.  The loads of a wavefront
-    // complete in order; with those behind B's stage c + 1 outstanding all of that stage has landed for it, the barrier extends that to
-    // all.  Past the end the loads fetch zeros, which keeps their number the same.  (Tiles with short stages need the depth: 1024 x 1152 x
-    // 9216 results of three planes each on 128 x 128 tiles, 0.7 us a stage with two stages in flight.)
-    auto load_panel = [&](auto ISA, int to_buf, int c) __attribute__((always_inline)) {
-        const Stage s = stage_at(c);
-#pragma unroll
-        for (int k = decltype(ISA)::value ? 0 : LA; k < (decltype(ISA)::value ? LA : NL); ++k) load_one(std::false_type(), to_buf, s, k);
-    };
-    constexpr int B0 = (D + 1) * Shape::PA, BE = B0 + D * Shape::PB;
-    for (int i = 0; i < D; ++i) {
-        load_panel(std::true_type(), i * Shape::PA, c0 + i);
-        load_panel(std::false_type(), B0 + i * Shape::PB, c0 + i);
-    }
-    FW_WAIT_VM((D - 1) * NL);
-    __builtin_amdgcn_s_barrier();
-    FW_COMPILER_FENCE();
-#pragma unroll
-    for (int f = 0; f < NF; ++f) read_one(at_a, B0 + at_b, 0, f);
     // the reads over the first three quarters of the matrix instructions (the last ones have to be back when the next half begins)
-    auto half_turn = [&](int ra, int rb, auto HALF, auto ISA, auto ALL, int to_buf, const Stage& next) __attribute__((always_inline)) {
-        constexpr int half = decltype(HALF)::value, K0 = decltype(ISA)::value ? 0 : LA, KN = decltype(ISA)::value ? LA : LB;
+    // LOADS: 0 none, 1 a panel of A, 2 of B
+    auto half_turn = [&](int ra, int rb, auto HALF, auto LOADS, auto ALL, int to_buf, const Stage& next) __attribute__((always_inline)) {
+        constexpr int half = decltype(HALF)::value, what = decltype(LOADS)::value;
+        constexpr int K0 = what == 1 ? 0 : LA, KN = what == 0 ? 0 : what == 1 ? LA : LB;
         static_for<0, NM>([&](auto M) __attribute__((always_inline)) {
             constexpr int m = decltype(M)::value;
 #pragma unroll
@@ -285,31 +258,106 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
                 if (r * (3 * NM) / (4 * NF) == m) read_one(ra, rb, half ^ 1, r);
 #pragma unroll
             for (int k = 0; k < KN; ++k)
-                if (k * NM / KN + (NM > KN) == m) load_one(ALL, to_buf, next, K0 + k);
+                if (k * NM / (KN ? KN : 1) + (NM > KN) == m) load_one(ALL, to_buf, next, K0 + k);
             multiply_one(half, m);
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    int a0 = 0, b0 = B0;                         // the stage's buffers
-    int c = c0;
-    auto turn = [&](auto ALL) __attribute__((always_inline)) {
-        const int a1 = a0 == D * Shape::PA ? 0 : a0 + Shape::PA, free_a = a0 == 0 ? D * Shape::PA : a0 - Shape::PA;
-        const int b1 = b0 == BE - Shape::PB ? B0 : b0 + Shape::PB;
-        const Stage next = stage_at(c + D);
-        half_turn(at_a + a0, at_b + b0, std::integral_constant<int, 0>(), std::true_type(), ALL, free_a, next);
-        FW_WAIT_LGKM0();
-        FW_WAIT_VM((D - 1) * LA + (D - 2) * LB);
+    if constexpr (!PLANES) {
+        // At the barrier in the middle of stage c every wavefront holds the stage's second half in registers, so its buffers are free: in the
+        // half that follows the loads of B's stage c + D go out, in the half after that those of A's stage c + D + 1.  The loads of a wavefront
+        // complete in order; with those behind B's stage c + 1 outstanding all of that stage has landed for it, the barrier extends that to
+        // all.  Past the end the loads fetch zeros, which keeps their number the same.  (Tiles with short stages need the depth: 1024 x 1152 x
+        // 9216 results of three planes each on 128 x 128 tiles, 0.7 us a stage with two stages in flight.)
+        auto load_panel = [&](auto ISA, int to_buf, int c) __attribute__((always_inline)) {
+            const Stage s = stage_at(c);
+#pragma unroll
+            for (int k = decltype(ISA)::value ? 0 : LA; k < (decltype(ISA)::value ? LA : NL); ++k) load_one(std::false_type(), to_buf, s, k);
+        };
+        constexpr int B0 = (D + 1) * Shape::PA, BE = B0 + D * Shape::PB;
+        for (int i = 0; i < D; ++i) {
+            load_panel(std::true_type(), i * Shape::PA, c0 + i);
+            load_panel(std::false_type(), B0 + i * Shape::PB, c0 + i);
+        }
+        FW_WAIT_VM((D - 1) * NL);
         __builtin_amdgcn_s_barrier();
         FW_COMPILER_FENCE();
-        half_turn(at_a + a1, at_b + b1, std::integral_constant<int, 1>(), std::false_type(), ALL, b0, next);
-        a0 = a1; b0 = b1;
-        ++c;
-    };
-    while (c < cend) {
-        // stages up to `fast` ask for whole ones only
-        const int fast = (PLANES ? cend : min(cend, BKM && c + D >= g.part ? g.part + whole : min(whole, g.part))) - D;
-        while (c < fast) turn(std::true_type());
-        turn(std::false_type());
+#pragma unroll
+        for (int f = 0; f < NF; ++f) read_one(at_a, B0 + at_b, 0, f);
+        int a0 = 0, b0 = B0;                         // the stage's buffers
+        int c = c0;
+        auto turn = [&](auto ALL) __attribute__((always_inline)) {
+            const int a1 = a0 == D * Shape::PA ? 0 : a0 + Shape::PA, free_a = a0 == 0 ? D * Shape::PA : a0 - Shape::PA;
+            const int b1 = b0 == BE - Shape::PB ? B0 : b0 + Shape::PB;
+            const Stage next = stage_at(c + D);
+            half_turn(at_a + a0, at_b + b0, std::integral_constant<int, 0>(), std::integral_constant<int, 1>(), ALL, free_a, next);
+            FW_WAIT_LGKM0();
+            FW_WAIT_VM((D - 1) * LA + (D - 2) * LB);
+            __builtin_amdgcn_s_barrier();
+            FW_COMPILER_FENCE();
+            half_turn(at_a + a1, at_b + b1, std::integral_constant<int, 1>(), std::integral_constant<int, 2>(), ALL, b0, next);
+            a0 = a1; b0 = b1;
+            ++c;
+        };
+        while (c < cend) {
+            // stages up to `fast` ask for whole ones only
+            const int fast = min(cend, BKM && c + D >= g.part ? g.part + whole : min(whole, g.part)) - D;
+            while (c < fast) turn(std::true_type());
+            turn(std::false_type());
+        }
+    } else {
+        // A panel of the next stage is asked for when its plane was used last in this one, over two halves where two planes end
+        // together.  vmcnt: what may be outstanding is what was asked for behind the panel that the next product needs.
+        using std::integral_constant;
+        constexpr integral_constant<int, 0> H0, NONE;
+        constexpr integral_constant<int, 1> H1, PANEL_A;
+        constexpr integral_constant<int, 2> PANEL_B;
+        constexpr std::true_type ALL;
+        constexpr int AH = 0, AM = Shape::PA, AL = 2 * Shape::PA, BH = 3 * Shape::PA, BM = BH + Shape::PB, BL = BM + Shape::PB;
+        auto plane = [&](Stage s, int p) __attribute__((always_inline)) { s.a += p * g.aplane; s.b += p * g.bplane; return s; };     // 0 h, 1 m, 2 l
+        auto load_panel = [&](auto A, int buf, const Stage& s) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = decltype(A)::value ? 0 : LA; k < (decltype(A)::value ? LA : NL); ++k) load_one(ALL, buf, s, k);
+        };
+        const Stage first = stage_at(c0);
+        load_panel(std::true_type(), AL, plane(first, 2));
+        load_panel(std::false_type(), BH, first);
+        load_panel(std::true_type(), AM, plane(first, 1));
+        load_panel(std::false_type(), BM, plane(first, 1));
+        load_panel(std::true_type(), AH, first);
+        load_panel(std::false_type(), BL, plane(first, 2));
+        auto meet = [&](auto VM) __attribute__((always_inline)) {
+            FW_WAIT_LGKM0();
+            FW_WAIT_VM(decltype(VM)::value);
+            __builtin_amdgcn_s_barrier();
+            FW_COMPILER_FENCE();
+        };
+        meet(integral_constant<int, 2 * LA + 2 * LB>());
+#pragma unroll
+        for (int f = 0; f < NF; ++f) read_one(at_a + AL, at_b + BH, 0, f);
+        Stage now = first;
+        for (int c = c0; c < cend; ++c) {
+            const Stage next = stage_at(min(c + 1, cend - 1));       // past the end the last stage once more, unread
+            half_turn(at_a + AL, at_b + BH, H0, PANEL_B, ALL, BL, plane(now, 2));             // l h; the loads are of this stage (see below)
+            meet(integral_constant<int, LA + 2 * LB>());                                      // m
+            half_turn(at_a + AM, at_b + BH, H1, PANEL_A, ALL, AL, plane(next, 2));
+            half_turn(at_a + AM, at_b + BH, H0, NONE, ALL, 0, next);                          // m h
+            meet(integral_constant<int, LA + LB>());                                          // h of A
+            half_turn(at_a + AH, at_b + BH, H1, NONE, ALL, 0, next);
+            half_turn(at_a + AH, at_b + BH, H0, NONE, ALL, 0, next);                          // h h
+            meet(integral_constant<int, LA + LB>());                                          // (m of B is older than h of A)
+            half_turn(at_a + AH, at_b + BM, H1, PANEL_B, ALL, BH, next);
+            half_turn(at_a + AH, at_b + BM, H0, NONE, ALL, 0, next);                          // h m
+            FW_WAIT_LGKM0();
+            half_turn(at_a + AM, at_b + BM, H1, NONE, ALL, 0, next);
+            half_turn(at_a + AM, at_b + BM, H0, NONE, ALL, 0, next);                          // m m
+            meet(integral_constant<int, LA + LB>());                                          // l of B
+            half_turn(at_a + AH, at_b + BL, H1, PANEL_A, ALL, AM, plane(next, 1));
+            half_turn(at_a + AH, at_b + BL, H0, PANEL_B, ALL, BM, plane(next, 1));            // h l
+            meet(integral_constant<int, LA + LB>());                                          // the next stage's l of A and h of B
+            half_turn(at_a + AL, at_b + BH, H1, PANEL_A, ALL, AH, next);
+            now = next;
+        }
     }
     FW_WAIT_VM(0);
     FW_WAIT_LGKM0();
@@ -382,20 +430,21 @@ __device__ __forceinline__ void tile_vector(const float* p, int s, int cols, flo
 
 // Tile shape and runs of the least estimated time in cycles: rounds of 256 workgroups x (stages + filling the ring) x the longer of a stage's
 // matrix instructions and its loads (about 30 bytes per cycle and compute unit), plus the pass that adds the runs.  Runs are for the tiles
-// behind whole rounds, and keep at least 4 stages.
-inline void tile_plan(TileProduct& g, bool pair) {
+// behind whole rounds, and keep at least 4 stages (of planes: 2, each with six products).
+inline void tile_plan(TileProduct& g, bool pair, bool planes = false) {
     static const int shapes[][2] = {{4, 4}, {2, 4}, {2, 2}, {1, 4}, {1, 2}};
     double best = 1e300;
-    for (const auto& s : shapes) {
-        const int nrt = s[0], nct = s[1], tc = pair ? 32 * nct : 64 * nct;
+    for (int i = planes ? 1 : 0; i < 5; ++i) {               // the planes of 256 x 256 results do not fit into LDS
+        const int nrt = shapes[i][0], nct = shapes[i][1], tc = pair ? 32 * nct : 64 * nct;
         const int nrb = (g.R + 64 * nrt - 1) / (64 * nrt), ncb = (g.C + tc - 1) / tc;
         const long long tiles = (long long)nrb * ncb;
-        const double t_mfma = 128.0 * nrt * nct + 60.0, t_load = (nrt + nct) * 8192.0 / 30.0, t_stage = t_mfma > t_load ? t_mfma : t_load;
+        const double t_mfma = 128.0 * nrt * nct * (planes ? 6 : 1) + 60.0, t_load = (nrt + nct) * 8192.0 / 30.0 * (planes ? 3 : 1);
+        const double t_stage = t_mfma > t_load ? t_mfma : t_load, fill = planes ? 1.5 : 4.0;
         const int rest = (int)(tiles % 256);
-        for (int runs = 1; runs <= 32 && (runs == 1 || (rest > 0 && rest * runs <= 512 && g.stages / runs >= 4)); ++runs) {
+        for (int runs = 1; runs <= 32 && (runs == 1 || (rest > 0 && rest * runs <= 512 && g.stages / runs >= (planes ? 2 : 4))); ++runs) {
             const int spr = (g.stages + runs - 1) / runs, n = (g.stages + spr - 1) / spr;
-            double cost = (double)((n > 1 ? tiles : tiles + 255) / 256) * (g.stages + 4.0) * t_stage;
-            if (n > 1) cost += (double)((rest * n + 255) / 256) * (spr + 4.0) * t_stage + 6000.0 + 2.0 * n * rest * (nrt * nct * 16384.0) / 4e12 * 2.1e9;
+            double cost = (double)((n > 1 ? tiles : tiles + 255) / 256) * (g.stages + fill) * t_stage;
+            if (n > 1) cost += (double)((rest * n + 255) / 256) * (spr + fill) * t_stage + 6000.0 + 2.0 * n * rest * (nrt * nct * 16384.0) / 4e12 * 2.1e9;
             if (cost < best * 0.999) {
                 best = cost;
                 g.nrt = nrt; g.nct = nct; g.nrb = nrb; g.ncb = ncb; g.runs = n; g.spr = spr;
@@ -421,7 +470,8 @@ fw_status tile_launch(const TileProduct& g, const Epi& epi, hipStream_t st) {
 
 template <TileKind KIND, bool AKM, bool BKM, bool PAIR, class Epi>
 fw_status tile_product(const TileProduct& g, const Epi& epi, hipStream_t st) {
-    if (g.nrt == 4) return tile_launch<KIND, 4, 4, 8, AKM, BKM, PAIR>(g, epi, st);
+    if constexpr (KIND != TILE_PLANES)
+        if (g.nrt == 4) return tile_launch<KIND, 4, 4, 8, AKM, BKM, PAIR>(g, epi, st);
     if (g.nrt == 2 && g.nct == 4) return tile_launch<KIND, 2, 4, 8, AKM, BKM, PAIR>(g, epi, st);
     if (g.nrt == 2) return tile_launch<KIND, 2, 2, 8, AKM, BKM, PAIR>(g, epi, st);
     if (g.nct == 4) return tile_launch<KIND, 1, 4, 8, AKM, BKM, PAIR>(g, epi, st);
