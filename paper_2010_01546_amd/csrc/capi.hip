@@ -314,7 +314,9 @@ fw_status fw_whiten_evd(const float* Phi_x, int M, const fw_evd_params* p, float
 
 fw_status fw_rms_norm(const void* X, const void* R, fw_dtype dt, int N, int M, const float* w, float eps, void* H, void* Y, signed char* q,
                       float* qs, void* stream) {
-    if (!X || (!Y && !q) || !q != !qs || !(eps > 0.f) || (Y && (Y == X || Y == R || Y == H))) return FW_ERR_INVALID_ARG;
+    const void* q8 = q;
+    if (!X || (!Y && !q) || !q != !qs || !(eps > 0.f) || (Y && (Y == X || Y == R || Y == H)) || (q && (q8 == X || q8 == R || q8 == H || q8 == Y)))
+        return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, 1);
     if (rc != FW_OK) return rc;
     if (!all_aligned16(X, R, w, H, Y, q, qs)) return FW_ERR_ALIGNMENT;
@@ -345,8 +347,8 @@ fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, cons
 fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* Z, const void* dH,
                         const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws, size_t ws_bytes, void* stream) {
     if (!X || !Wg || !Wu || !Z || !dH || !dWg != !dWu || !dbg != !dbu || (!dX && !dWg && !dbg)) return FW_ERR_INVALID_ARG;
-    if (dX && (dX == X || dX == dH || dX == (const void*)Z)) return FW_ERR_INVALID_ARG;
-    if (dWg && (dWg == dWu || dWg == Wg || dWg == Wu || dWu == Wg || dWu == Wu)) return FW_ERR_INVALID_ARG;
+    if (dX && (dX == X || dX == dH || dX == (const void*)Z || dX == Wg || dX == Wu || dX == dWg || dX == dWu)) return FW_ERR_INVALID_ARG;
+    if (dWg && (dWg == dWu || dWg == Wg || dWg == Wu || dWu == Wg || dWu == Wu || dWg == X || dWu == X)) return FW_ERR_INVALID_ARG;
     if (dbg && dbg == dbu) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, S);
     if (rc != FW_OK) return rc;

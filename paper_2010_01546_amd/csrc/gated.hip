@@ -34,8 +34,8 @@ template <int ACT> __device__ __forceinline__ void activation(float g, float& a,
         a = g * p;
         da = p + 2.f * g * p * (1.f - p) * k * (1.f + 0.134145f * g * g);
     } else {
-        a = g > 0.f ? g : 0.f;
-        da = g > 0.f ? 1.f : 0.f;
+        a = g <= 0.f ? 0.f : g;               // NaN stays NaN
+        da = g <= 0.f ? 0.f : g > 0.f ? 1.f : g;
     }
 }
 template <class F> __device__ __forceinline__ void with_activation(int act, const F& f) {

@@ -317,6 +317,142 @@ def test_int8_product(N, M, S, dtype):
     within(Y.host(), want, 4 * U32 * (plain + (0 if bias is None else np.abs(bias))) + HALF[dtype] * np.abs(want))
 
 
+@pytest.mark.parametrize("N,M,S", [(2100, 520, 4200), (2304, 192, 4608)])
+def test_many_tiles(N, M, S):
+    """More tiles than compute units: whole rounds of them, and a rest that is cut into runs; bfloat16 and 8 bits."""
+    t, dt = torch.bfloat16, b.FW_BF16
+    rng, X, Wg, Wu, bg, bu = gated_inputs(N, M, S, "bf16", True)
+    H, Z = run_forward(X, Wg, Wu, bg, bu, "silu", "bf16")
+    check_forward(H.host(), Z.host(), X, Wg, Wu, bg, bu, "silu", "bf16")
+    dH, mu = rows(rng, N, S, "bf16", 0.1), lo.f64(X).mean(0).astype(np.float32)
+    dX, dWg, dWu = Out(N, M, dtype=t), Out(S, M, dtype=t), Out(S, M, dtype=t)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_GRAD, M, S, b.conv_desc(N, M), dt))
+    ws.fill_(255)
+    b.fw_gated_grad(dev(X, t), dt, N, M, S, dev(Wg, t), dev(Wu, t), Z.t, dev(dH, t), dev(mu), dX.t, dWg.t, dWu.t, None, None, ws)
+    torch.cuda.synchronize()
+    Zh = Z.host()
+    dg, du = rounded_product(dH, Zh[0], "bf16"), rounded_product(dH, Zh[1], "bf16")
+    want, half = lo.gated_grad_from(dg, du, X, Wg, Wu, mu), HALF["bf16"]
+    ag, au, aX = np.abs(dg), np.abs(du), np.abs(lo.f64(X)) + np.abs(mu)
+    within(dX.host(), want[0], (2 * S + 8) * U32 * (ag @ np.abs(lo.f64(Wg)) + au @ np.abs(lo.f64(Wu))) + half * np.abs(want[0]), "dX")
+    within(dWg.host(), want[1], (2 * N + 8) * U32 * (ag.T @ aX) + half * np.abs(want[1]), "dWg")
+    within(dWu.host(), want[2], (2 * N + 8) * U32 * (au.T @ aX) + half * np.abs(want[2]), "dWu")
+    Xq, Wq = rng.integers(-128, 128, (N, M)).astype(np.int8), rng.integers(-128, 128, (2 * S, M)).astype(np.int8)
+    sx, sw, Y = np.full(N, 0.01, np.float32), np.full(2 * S, 0.02, np.float32), Out(N, 2 * S, dtype=torch.float32)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_INT8_PRODUCT, M, 2 * S, b.conv_desc(N, M)))
+    b.fw_int8_product(dev(Xq, torch.int8), dev(sx), N, M, 2 * S, dev(Wq, torch.int8), dev(sw), None, Y.t, b.FW_F32, ws)
+    torch.cuda.synchronize()
+    want = lo.int8_product(Xq, sx, Wq, sw)
+    within(Y.host(), want, 4 * U32 * np.abs(want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M,S", [(3, 70, 90), (70, 72, 100), (150, 129, 200)])
+def test_gated_with_infinite_and_nan_entries(N, M, S, dtype):
+    """They reach the results that the formula lets them reach, as the same infinities and NaN, and no others."""
+    t, dt = TDT[dtype], FDT[dtype]
+    rng, X, Wg, Wu, bg, bu = gated_inputs(N, M, S, dtype, True)
+    X, Wg = X.copy(), Wg.copy()
+    X[1, 5], X[2, M - 1] = np.inf, np.nan
+    Wg[S - 1, 3] = -np.inf
+    H, Z = run_forward(X, Wg, Wu, bg, bu, "relu", dtype)
+    with np.errstate(all="ignore"):
+        want = lo.gated(X, Wg, Wu, "relu", bg, bu)
+    got = H.host()
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isfinite(got), fine)
+    assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+    assert fine[0, :S - 1].all() and not fine[1].all() and np.isnan(got[2]).all()
+    assert relF(got[fine], want[fine]) < (2 * HALF["bf16"] if dtype == "bf16" else 1e-5)
+    # gradient: finite factors, infinite entries of dH, X and the weights
+    X[2, M - 1] = 0.5
+    Zf = (0.3 + np.abs(rng.standard_normal((2, N, S)))).astype(np.float32)
+    dH = rows(rng, N, S, dtype, 0.1)
+    dH[0, 7], dH[2, 8] = np.inf, np.nan
+    dX, dWg, dWu = Out(N, M, dtype=t), Out(S, M, dtype=t), Out(S, M, dtype=t)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_GRAD, M, S, b.conv_desc(N, M), dt))
+    ws.fill_(255)
+    b.fw_gated_grad(dev(X, t), dt, N, M, S, dev(Wg, t), dev(Wu, t), dev(Zf), dev(dH, t), None, dX.t, dWg.t, dWu.t, None, None, ws)
+    torch.cuda.synchronize()
+    with np.errstate(all="ignore"):
+        dg, du = rounded_product(dH, lo.f64(Zf[0]), dtype), rounded_product(dH, lo.f64(Zf[1]), dtype)
+        want = lo.gated_grad_from(dg, du, X, Wg, Wu)
+    for got, w, what in zip((dX.host(), dWg.host(), dWu.host()), want, ("dX", "dWg", "dWu")):
+        fine = np.isfinite(w)
+        assert np.array_equal(np.isfinite(got), fine), what
+        assert np.array_equal(got[np.isinf(w)], w[np.isinf(w)]), what
+        assert fine.any() and relF(got[fine], w[fine]) < (2 * HALF["bf16"] if dtype == "bf16" else 1e-5), what
+
+
+def test_offsets_beyond_32_bits():
+    """Rows at the end of tensors of more than 2^31 entries."""
+    t, dt = torch.bfloat16, b.FW_BF16
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    N, M = 70000, 32768
+    X = torch.randn(N, M, generator=gen, device=DEV, dtype=t)
+    Y, q, qs = torch.empty_like(X), torch.empty(N, M, dtype=torch.int8, device=DEV), torch.empty(N, device=DEV)
+    b.fw_rms_norm(X, None, dt, N, M, None, EPS, None, Y, q, qs)
+    torch.cuda.synchronize()
+    at = [0, 65535, N - 1]
+    want = lo.rms_norm(X[at].float().cpu().numpy(), None, EPS)
+    within(Y[at].float().cpu().numpy().astype(np.float64), want, np.abs(want) * (HALF["bf16"] + 4 * U32))
+    within(q[at].cpu().numpy().astype(np.float64), lo.int8_steps(want)[0], 0.5 + 1e-9)
+    del X, Y, q, qs
+    N, M, S = 36000, 64, 65536
+    X = torch.randn(N, M, generator=gen, device=DEV).to(t)
+    Wg, Wu = ((torch.randn(S, M, generator=gen, device=DEV) / 8).to(t) for _ in range(2))
+    H, Z, d = torch.empty(N, S, dtype=t, device=DEV), torch.empty(2, N, S, device=DEV), b.conv_desc(N, M)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_FORWARD, M, S, d, dt))
+    b.fw_gated_forward(X, dt, N, M, S, Wg, Wu, None, None, b.FW_ACT_SILU, H, Z, ws)
+    torch.cuda.synchronize()
+    num = lambda x: x.float().cpu().numpy().astype(np.float64)  # noqa: E731
+    for n in (0, N // 2, N - 1):
+        check_forward(num(H[n:n + 1]), num(Z[:, n:n + 1]), num(X[n:n + 1]), num(Wg), num(Wu), None, None, "silu", "bf16")
+    dH = H                                                            # any gradient will do
+    dX, dWg, dWu = torch.empty_like(X), torch.empty_like(Wg), torch.empty_like(Wu)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_GRAD, M, S, d, dt))
+    b.fw_gated_grad(X, dt, N, M, S, Wg, Wu, Z, dH, None, dX, dWg, dWu, None, None, ws)
+    torch.cuda.synchronize()
+    n = N - 1
+    D = [lo.f64((dH[n].float() * Z[k, n]).to(t).float().cpu().numpy()) for k in range(2)]
+    want = D[0] @ num(Wg) + D[1] @ num(Wu)
+    mag = np.abs(D[0]) @ np.abs(num(Wg)) + np.abs(D[1]) @ np.abs(num(Wu))
+    within(num(dX[n]), want, (2 * S + 8) * U32 * mag + HALF["bf16"] * np.abs(want), "dX")
+    s = [0, S // 2 + 1, S - 1]
+    for k, got in ((0, dWg), (1, dWu)):
+        D = num((dH[:, s].float() * Z[k][:, s]).to(t))
+        want, mag = D.T @ num(X), np.abs(D).T @ np.abs(num(X))
+        within(num(got[s]), want, (2 * N + 8) * U32 * mag + HALF["bf16"] * np.abs(want), "dW")
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with its own workspace, give what they give alone."""
+    N, M, S, t, dt = 640, 512, 1536, torch.bfloat16, b.FW_BF16
+    d, inputs = b.conv_desc(N, M), []
+    for seed in (1, 2):
+        rng = np.random.default_rng(seed)
+        inputs.append([dev(rows(rng, *s, "bf16", 0.1), t) for s in ((N, M), (S, M), (S, M), (N, S))])
+
+    def call(k, stream):
+        X, Wg, Wu, dH = inputs[k]
+        o = dict(H=torch.empty(N, S, dtype=t, device=DEV), Z=torch.empty(2, N, S, device=DEV), dX=torch.empty_like(X), dWg=torch.empty_like(Wg), dWu=torch.empty_like(Wu))
+        w = [workspace(b.fw_workspace_bytes(op, M, S, d, dt)) for op in (b.FW_OP_GATED_FORWARD, b.FW_OP_GATED_GRAD)]
+        torch.cuda.synchronize() if stream is None else None
+        b.fw_gated_forward(X, dt, N, M, S, Wg, Wu, None, None, b.FW_ACT_SILU, o["H"], o["Z"], w[0], stream=stream)
+        b.fw_gated_grad(X, dt, N, M, S, Wg, Wu, o["Z"], dH, None, o["dX"], o["dWg"], o["dWu"], None, None, w[1], stream=stream)
+        return o, w
+
+    alone = [call(k, None) for k in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for turn in range(3):
+        both = [call(k, streams[k]) for k in range(2)]
+        torch.cuda.synchronize()
+        for k in range(2):
+            for name in alone[k][0]:
+                assert torch.equal(alone[k][0][name], both[k][0][name]), (turn, k, name)
+
+
 # -------------------------------------------------------------------------------------------- as they are used together
 
 def whitened_step(dtype, stream=None):

@@ -76,7 +76,7 @@ def test_norm_refusals():
     statuses(L.fw_rms_norm, good, [
         (dict(X=None), I), (dict(Y=None, q=None, qs=None), I), (dict(q=None), I), (dict(qs=None), I), (dict(eps=0.0), I), (dict(eps=-1.0), I),
         (dict(eps=float("nan")), I), (dict(N=0), I), (dict(N=-3), I), (dict(M=0), I), (dict(dt=2), I), (dict(Y=p(1)), I), (dict(Y=p(2)), I),
-        (dict(Y=p(4)), I), (dict(M=32769), U), (dict(N=(1 << 21) + 1), U), (dict(X=p(1) + 8), A), (dict(qs=p(7) + 4), A), (dict(w=p(3) + 4), A)])
+        (dict(Y=p(4)), I), (dict(q=p(1)), I), (dict(q=p(4)), I), (dict(q=p(5)), I), (dict(M=32769), U), (dict(N=(1 << 21) + 1), U), (dict(X=p(1) + 8), A), (dict(qs=p(7) + 4), A), (dict(w=p(3) + 4), A)])
     good = dict(H=p(1), dt=1, N=4, M=8, w=p(3), eps=1e-5, dY=p(2), dH=p(4), dX=p(5), dw=p(6), ws=p(7), n=1 << 20, stream=None)
     statuses(L.fw_rms_norm_grad, good, [
         (dict(H=None), I), (dict(dY=None), I), (dict(dX=None, dw=None), I), (dict(eps=0.0), I), (dict(dX=p(1)), I), (dict(N=0), I), (dict(dt=-1), I),
@@ -102,7 +102,7 @@ def test_gated_refusals():
     statuses(L.fw_gated_grad, good, [
         (dict(X=None), I), (dict(Wg=None), I), (dict(Wu=None), I), (dict(Z=None), I), (dict(dH=None), I), (dict(dWg=None), I), (dict(dWu=None), I),
         (dict(dbg=None), I), (dict(dbu=None), I), (dict(dX=None, dWg=None, dWu=None, dbg=None, dbu=None), I), (dict(dX=p(1)), I), (dict(dX=p(5)), I),
-        (dict(dX=p(4)), I), (dict(dWg=p(8)), I), (dict(dWg=p(2)), I), (dict(dWu=p(2)), I), (dict(dbu=p(9)), I), (dict(dt=2), I), (dict(N=0), I),
+        (dict(dX=p(4)), I), (dict(dWg=p(8)), I), (dict(dWg=p(2)), I), (dict(dWu=p(2)), I), (dict(dWu=p(1)), I), (dict(dX=p(7)), I), (dict(dX=p(2)), I), (dict(dbu=p(9)), I), (dict(dt=2), I), (dict(N=0), I),
         (dict(S=0), I), (dict(M=40000), U), (dict(S=70000), U), (dict(mu=p(12) + 4), A), (dict(dX=p(6) + 2), A), (dict(ws=None), W), (dict(n=64), W)])
 
 
