@@ -32,7 +32,8 @@ template <int ACT> __device__ __forceinline__ void activation(float g, float& a,
         // (1 + tanh z) / 2 = sigmoid(2 z)
         const float k = 0.79788456080286536f, p = sigmoid(2.f * k * (g + 0.044715f * g * g * g));
         a = g * p;
-        da = p + 2.f * g * p * (1.f - p) * k * (1.f + 0.134145f * g * g);
+        const float c = fminf(fmaxf(g, -64.f), 64.f);        // p (1 - p) is zero beyond; g^2 may be infinite
+        da = p + 2.f * c * p * (1.f - p) * k * (1.f + 0.134145f * c * c);
     } else {
         a = g <= 0.f ? 0.f : g;               // NaN stays NaN
         da = g <= 0.f ? 0.f : g > 0.f ? 1.f : g;
@@ -442,12 +443,12 @@ ForwardWs forward_ws(fw_dtype dt, int N, int M, int S, void* ws) {
             w.Wg = c.take(plane3_bytes(S, M));
             w.Wu = c.take(plane3_bytes(S, M));
         }
-    } else if (M % 8) {
+    } else if (M % 8 && N > TILE_FEW) {
         w.X = c.take((size_t)N * up8(M) * 2);
         w.Wg = c.take((size_t)S * up8(M) * 2);
         w.Wu = c.take((size_t)S * up8(M) * 2);
     }
-    if (dt == FW_BF16 || N > FEW) w.partial = c.take(tile_partial_bytes(forward_plan(dt, N, M, S)));
+    if (N > (dt == FW_BF16 ? TILE_FEW : FEW)) w.partial = c.take(tile_partial_bytes(forward_plan(dt, N, M, S)));
     w.total = c.used;
     return w;
 }
@@ -503,6 +504,8 @@ fw_status forward_f32(const float* X, int N, int M, int S, const float* Wg, cons
 fw_status forward_bf16(const void* X, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu, fw_act act,
                        void* H, float* Z, void* ws, hipStream_t st) {
     const ForwardWs w = forward_ws(FW_BF16, N, M, S, ws);
+    const GateEpilogue<__bf16> epi = {reinterpret_cast<__bf16*>(H), Z, bg, bu, N, S, (int)act};
+    if (N <= TILE_FEW) return few_product<TILE_BF16, true>({bytes(X), bytes(Wg), bytes(Wu), N, S, 2 * M}, epi, st);
     if (M % 8) {             // 16-byte loads need aligned rows
         PadList pads;
         pads.add(X, N, w.X);
@@ -516,17 +519,18 @@ fw_status forward_bf16(const void* X, int N, int M, int S, const void* Wg, const
     g.a = bytes(X); g.b0 = bytes(Wg); g.b1 = bytes(Wu);
     g.apitch = g.bpitch = 2ll * up8(M);
     g.partial = w.partial;
-    return tile_product<TILE_BF16, false, false, true>(g, GateEpilogue<__bf16>{reinterpret_cast<__bf16*>(H), Z, bg, bu, N, S, (int)act}, st);
+    return tile_product<TILE_BF16, false, false, true>(g, epi, st);
 }
 
 template <class T>
-fw_status gate_grad(const T* dH, const float* Z, int N, int S, const GradWs& w, bool sums, T* dbg, T* dbu, hipStream_t st) {
+fw_status gate_grad(const T* dH, const float* Z, int N, int S, const GradWs& w, bool rounded, T* dbg, T* dbu, hipStream_t st) {
     const int Sp = up64(S);
+    const bool sums = rounded || dbg;
     hipLaunchKernelGGL(gate_grad_kernel<T>, dim3((Sp + 255) / 256, row_blocks(N, S)), dim3(256), 0, st, dH, Z, N, up64(N), S, Sp,
                        grad_rows(N, S), reinterpret_cast<__bf16*>(w.D), sums ? w.part : nullptr);
     FW_LAUNCH_CHECK();
     if (!sums) return FW_OK;
-    hipLaunchKernelGGL(bias_grad_kernel<T>, dim3(4 * Sp / 64), dim3(1024), 0, st, w.part, row_blocks(N, S), S, Sp, w.sums, dbg, dbu);
+    hipLaunchKernelGGL(bias_grad_kernel<T>, dim3((rounded ? 4 : 2) * Sp / 64), dim3(1024), 0, st, w.part, row_blocks(N, S), S, Sp, w.sums, dbg, dbu);
     FW_LAUNCH_CHECK();
     return FW_OK;
 }
@@ -535,7 +539,7 @@ fw_status grad_f32(const float* X, int N, int M, int S, const float* Wg, const f
                    float* dX, float* dWg, float* dWu, float* dbg, float* dbu, void* ws, hipStream_t st) {
     const GradWs w = grad_ws(FW_F32, N, M, S, ws);
     const int Sp = up64(S), Np = up64(N);
-    fw_status rc = gate_grad<float>(dH, Z, N, S, w, dbg != nullptr, dbg, dbu, st);
+    fw_status rc = gate_grad<float>(dH, Z, N, S, w, false, dbg, dbu, st);
     if (rc != FW_OK) return rc;
     const GradInputs in = {X, Wg, Wu, Z, dH, mu, N, M, S};
     Split s = {};
@@ -569,7 +573,7 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
                     __bf16* dX, __bf16* dWg, __bf16* dWu, __bf16* dbg, __bf16* dbu, void* ws, hipStream_t st) {
     const GradWs w = grad_ws(FW_BF16, N, M, S, ws);
     const int Sp = up64(S);
-    fw_status rc = gate_grad<__bf16>(dH, Z, N, S, w, dbg || (mu && dWg), dbg, dbu, st);
+    fw_status rc = gate_grad<__bf16>(dH, Z, N, S, w, mu && dWg, dbg, dbu, st);
     if (rc != FW_OK) return rc;
     if (M % 8) {
         PadList pads;

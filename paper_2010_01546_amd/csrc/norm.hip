@@ -237,20 +237,20 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void rms_grad_kernel(const T* __
             if ((threadIdx.x & 63) == 0) { red[turn][wave][0] = ss; red[turn][wave][1] = dot; }
             __syncthreads();
             ss = dot = 0.0;
-    #pragma unroll
-        for (int i = 0; i < G / 64; ++i) { ss += red[turn][i][0]; dot += red[turn][i][1]; }
+#pragma unroll
+            for (int i = 0; i < G / 64; ++i) { ss += red[turn][i][0]; dot += red[turn][i][1]; }
         }
         const double rho = 1.0 / sqrt(ss / (double)M + (double)eps);
-        const float rf = (float)rho, cf = (float)(rho * rho * rho * dot / (double)M);
+        const float rf = (float)rho, cf = (float)(rho * rho * dot / (double)M);      // rho^3 may lie outside float32
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int m = 8 * (t + G * j);
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float hv = h[j].get(i), vv = v[j].get(i);
-                sum[j][i] += vv * (hv * rf);
-                x[i] = rf * (vv * f[j].get(i)) - hv * cf;
+                const float hr = h[j].get(i) * rf, vv = v[j].get(i);
+                sum[j][i] += vv * hr;
+                x[i] = rf * (vv * f[j].get(i)) - hr * cf;
                 if (dH) x[i] += d[j].get(i);
             }
             if (dX && m < M) Place<END>(m, M).store(dX + at, x);

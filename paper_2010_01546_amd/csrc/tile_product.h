@@ -246,8 +246,8 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
                                                                   __builtin_bit_cast(bf16x8, fr[half][ta]), acc[ta][tb], 0, 0, 0);
     };
 
-    // the reads over the first three quarters of the matrix instructions (the last ones have to be back when the next half begins)
-    // LOADS: 0 none, 1 a panel of A, 2 of B
+    // The reads go over the first three quarters of the matrix instructions (the last ones have to be back when the next half begins).
+    // LOADS: 0 none, 1 a panel of A, 2 of B.
     auto half_turn = [&](int ra, int rb, auto HALF, auto LOADS, auto ALL, int to_buf, const Stage& next) __attribute__((always_inline)) {
         constexpr int half = decltype(HALF)::value, what = decltype(LOADS)::value;
         constexpr int K0 = what == 1 ? 0 : LA, KN = what == 0 ? 0 : what == 1 ? LA : LB;
@@ -267,8 +267,8 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
         // At the barrier in the middle of stage c every wavefront holds the stage's second half in registers, so its buffers are free: in the
         // half that follows the loads of B's stage c + D go out, in the half after that those of A's stage c + D + 1.  The loads of a wavefront
         // complete in order; with those behind B's stage c + 1 outstanding all of that stage has landed for it, the barrier extends that to
-        // all.  Past the end the loads fetch zeros, which keeps their number the same.  (Tiles with short stages need the depth: 1024 x 1152 x
-        // 9216 results of three planes each on 128 x 128 tiles, 0.7 us a stage with two stages in flight.)
+        // all.  Past the end the loads fetch zeros, which keeps their number the same.  (Small tiles gain from a deep ring: 501 x 2304 x
+        // 6145, two projections, 39.7 us with two stages, 36.6 with four.)
         auto load_panel = [&](auto ISA, int to_buf, int c) __attribute__((always_inline)) {
             const Stage s = stage_at(c);
 #pragma unroll
@@ -476,6 +476,126 @@ fw_status tile_product(const TileProduct& g, const Epi& epi, hipStream_t st) {
     if (g.nrt == 2) return tile_launch<KIND, 2, 2, 8, AKM, BKM, PAIR>(g, epi, st);
     if (g.nct == 4) return tile_launch<KIND, 1, 4, 8, AKM, BKM, PAIR>(g, epi, st);
     return tile_launch<KIND, 1, 2, 8, AKM, BKM, PAIR>(g, epi, st);
+}
+
+// ---- few rows: C[r][c] = sum_k A[r][k] B[c][k] for up to 16 rows, rows along the contraction and of any length.  Bound by the one read of B.
+// A workgroup owns `cols` columns (PAIR: of each matrix), so many that every compute unit gets as much of B to read; its wavefronts take
+// stages of 128 bytes in turn, two ahead in registers, turn them through 6 KB of LDS of their own (eight lanes load the 128 bytes of a
+// row, so that whole cache lines are asked for) and add up their sums at the end: one launch, no workspace, no padded copies.
+// Two projections of one row of 4608 bfloat16, 12288 columns: 42.7 us, 5.3 TB/s; 16 rows of 12288 bytes, 4608 columns: 11.6 us, 4.9 TB/s.
+// (Tiles of 64 rows whose contraction is cut into runs: 43.7 and 18.0 us; 1 x 1153, 1001 columns, whose rows these need padded: 13.3
+// against 5.9.  32 rows by two tiles of 16: from 4608 x 2304 on slower than tiles of 64.)
+constexpr int TILE_FEW = 16;
+struct FewProduct {
+    const char *a, *b0, *b1;
+    int N, C, bytes, cols;        // rows, columns (PAIR: of each matrix), bytes of a row, columns of a workgroup
+};
+template <TileKind KIND, bool PAIR, class Epi>
+__global__ __launch_bounds__(512, 4) void few_product_kernel(FewProduct g, Epi epi) {
+    constexpr bool I8 = KIND == TILE_I8;
+    constexpr int NW = 8;
+    using Acc = typename std::conditional<I8, intx4, floatx4>::type;
+    __shared__ __align__(16) char lds[NW][6144];                      // a wavefront's stage: 32 rows of B, 16 of A
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col0 = blockIdx.x * g.cols, cend = min(g.C, col0 + g.cols);
+    const int chunks = g.bytes / 16, stages = (g.bytes + 127) / 128;       // whole chunks of 16 bytes
+    // 48 rows of a stage, eight at a time: where they begin, behind addresses that are the same for the workgroup
+    const char *b0 = g.b0 + (size_t)col0 * g.bytes, *b1 = (PAIR ? g.b1 : g.b0) + (size_t)col0 * g.bytes;
+    unsigned at[6];
+#pragma unroll
+    for (int j = 0; j < 6; ++j) {
+        const int r = 8 * j + (lane >> 3);
+        at[j] = (unsigned)(j < 4 ? min(PAIR ? r & 15 : r, cend - 1 - col0) : min(r - 32, g.N - 1)) * g.bytes;
+    }
+    auto base = [&](int j) __attribute__((always_inline)) { return j < 2 ? b0 : j < 4 ? b1 : g.a; };
+    struct Stage { intx4 v[6]; };
+    auto load = [&](Stage& s, int c) __attribute__((always_inline)) {       // chunks outside of the rows: zeros
+        const bool in = c >= 0 && 8 * c + (lane & 7) < chunks;
+#pragma unroll
+        for (int j = 0; j < 6; ++j) __builtin_memcpy(&s.v[j], in ? base(j) + at[j] + 128 * c + 16 * (lane & 7) : reinterpret_cast<const char*>(&tile_zero), 16);
+    };
+    auto load_whole = [&](Stage& s, int c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 6; ++j) __builtin_memcpy(&s.v[j], base(j) + 128 * c + (at[j] + 16 * (lane & 7)), 16);
+    };
+    Acc acc[2] = {Acc{0, 0, 0, 0}, Acc{0, 0, 0, 0}};
+    // chunk c of row r at c ^ (r / 2 % 8).  A wavefront's accesses to LDS happen in their order; the fences keep the compiler to it.
+    auto use = [&](const Stage& s) __attribute__((always_inline)) {
+        FW_COMPILER_FENCE();
+#pragma unroll
+        for (int j = 0; j < 6; ++j)
+            *reinterpret_cast<intx4*>(&lds[wave][(8 * j + (lane >> 3)) * 128 + 16 * ((lane & 7) ^ ((4 * j + (lane >> 4)) & 7))]) = s.v[j];
+        FW_COMPILER_FENCE();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            intx4 fr[3];
+#pragma unroll
+            for (int f = 0; f < 3; ++f) fr[f] = *reinterpret_cast<const intx4*>(&lds[wave][(16 * f + l16) * 128 + 16 * ((4 * h + q) ^ (l16 >> 1))]);
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                if constexpr (I8) acc[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fr[f], fr[2], acc[f], 0, 0, 0);
+                else acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fr[f]), __builtin_bit_cast(bf16x8, fr[2]), acc[f], 0, 0, 0);
+            }
+        }
+    };
+    // from the end of the rows, whose last stage may not be whole, to their beginning
+    Stage s, t;
+    int c = stages - 1 - wave, more = c >= 0 ? c / NW - 1 : 0;       // stages behind the first two
+    load(s, c);
+    if (g.bytes % 16 && wave == 0) {                // the chunk that is not whole
+        const int n = 8 * c + (lane & 7) == chunks ? g.bytes - 16 * chunks : 0;
+        constexpr int E = I8 ? 1 : 2;
+#pragma unroll
+        for (int j = 0; j < 6; ++j) {
+            union { char b[16]; intx4 v; } u;
+            u.v = s.v[j];
+#pragma unroll
+            for (int i = 0; i < 16; i += E)
+                if (i < n) __builtin_memcpy(u.b + i, base(j) + at[j] + 16 * chunks + i, E);
+            s.v[j] = u.v;
+        }
+    }
+    load(t, c - NW);
+    for (c -= 2 * NW; more >= 2; more -= 2, c -= 2 * NW) {
+        use(s);
+        load_whole(s, c);
+        use(t);
+        load_whole(t, c - NW);
+    }
+    use(s);
+    if (more == 1) load_whole(s, c);
+    use(t);
+    if (more == 1) use(s);
+    // the wavefronts' sums, in order
+    FW_COMPILER_FENCE();
+#pragma unroll
+    for (int f = 0; f < 2; ++f) *reinterpret_cast<Acc*>(&lds[wave][1024 * f + 16 * lane]) = acc[f];
+    __syncthreads();
+    const auto total = [&](int f) __attribute__((always_inline)) {
+        Acc v = *reinterpret_cast<const Acc*>(&lds[0][1024 * f + 16 * lane]);
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            const Acc x = *reinterpret_cast<const Acc*>(&lds[w][1024 * f + 16 * lane]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += x[i];
+        }
+        return v;
+    };
+    if constexpr (PAIR) {
+        if (wave == 0 && col0 + 4 * q < cend) epi.apply(l16, col0 + 4 * q, total(0), total(1));
+    } else {
+        if (wave < 2 && col0 + 16 * wave + 4 * q < cend) epi.apply(l16, col0 + 16 * wave + 4 * q, total(wave));
+    }
+}
+template <TileKind KIND, bool PAIR, class Epi>
+fw_status few_product(FewProduct g, const Epi& epi, hipStream_t st) {
+    constexpr int MOST = PAIR ? 16 : 32;             // columns a workgroup can take
+    const int each = (g.C + 255) / 256, parts = (each + MOST - 1) / MOST;
+    g.cols = ((each + parts - 1) / parts + 3) / 4 * 4;
+    hipLaunchKernelGGL((few_product_kernel<KIND, PAIR, Epi>), dim3((g.C + g.cols - 1) / g.cols), dim3(512), 0, st, g, epi);
+    FW_LAUNCH_CHECK();
+    return FW_OK;
 }
 
 }  // namespace fw

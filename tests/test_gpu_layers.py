@@ -290,6 +290,65 @@ def test_gated_gradient(N, M, S, dtype):
         a.host()
 
 
+# few rows, where each workgroup has its columns' whole sums, and a few more: row ends of every kind, few and many columns
+FEW_SIZES = [(1, 7, 3), (2, 8, 259), (4, 33, 1), (15, 129, 300), (16, 577, 1030), (17, 1100, 33), (31, 136, 4100), (32, 2305, 6145), (3, 64, 8200),
+             (1, 12289, 20)]
+
+
+@pytest.mark.parametrize("N,M,S", FEW_SIZES)
+def test_gated_few_rows(N, M, S):
+    kind = act_of(N, M, S)
+    _, X, Wg, Wu, bg, bu = gated_inputs(N, M, S, "bf16", S % 2 == 0)
+    H, Z = run_forward(X, Wg, Wu, bg, bu, kind, "bf16")
+    check_forward(H.host(), Z.host(), X, Wg, Wu, bg, bu, kind, "bf16")
+    # the last weights of a row in front of entries that are no part of it: an infinite row of the weights reaches its own column alone
+    Wg[0] = np.inf
+    H2, _ = run_forward(X, Wg, Wu, bg, bu, kind, "bf16", keep=False)
+    assert torch.equal(H2.t[:, 1:], H.t[:, 1:])
+
+
+@pytest.mark.parametrize("N,M,S", FEW_SIZES)
+def test_int8_few_rows(N, M, S):
+    rng = np.random.default_rng(N + 13 * M + 7 * S)
+    Xq, Wq = rng.integers(-128, 128, (N, M)).astype(np.int8), rng.integers(-128, 128, (S, M)).astype(np.int8)
+    Y, ones = Out(N, S, dtype=torch.float32), torch.ones(max(N, S), device=DEV)
+    ws = b.fw_workspace_bytes(b.FW_OP_INT8_PRODUCT, M, S, b.conv_desc(N, M), b.FW_F32)
+    b.fw_int8_product(dev(Xq, torch.int8), ones, N, M, S, dev(Wq, torch.int8), ones, None, Y.t, b.FW_F32, workspace(ws) if ws else None)
+    torch.cuda.synchronize()
+    want = Xq.astype(np.int64) @ Wq.astype(np.int64).T
+    within(Y.host(), want.astype(np.float64), np.abs(want) * U32)
+
+
+def test_norm_gradient_of_extreme_rows():
+    """Rows whose rho^3 lies outside float32, on either side."""
+    rng = np.random.default_rng(5)
+    M, eps = 70, 1e-38
+    H = (rng.standard_normal((3, M)) * np.array([[1e25], [1.0], [1e-16]])).astype(np.float32)
+    dY = rng.standard_normal((3, M)).astype(np.float32)
+    dX = Out(3, M, dtype=torch.float32)
+    b.fw_rms_norm_grad(dev(H), b.FW_F32, 3, M, None, eps, dev(dY), None, dX.t, None)
+    torch.cuda.synchronize()
+    eps = float(np.float32(eps))
+    want = lo.rms_norm_grad(H, None, eps, dY)[0]
+    rho = 1 / np.sqrt(np.mean(lo.f64(H) ** 2, axis=1, keepdims=True) + eps)
+    first, second = np.abs(rho * dY), np.abs(H * rho ** 3 * np.mean(lo.f64(dY) * H, axis=1, keepdims=True))
+    within(dX.host(), want, U32 * np.abs(want) + 5 * U32 * (first + second), "dX")
+
+
+@pytest.mark.parametrize("kind", lo.ACTS)
+def test_gated_with_extreme_gates(kind):
+    """g as large as its type allows: the value is g or zero, the slope one or zero."""
+    X = np.ones((2, 1), dtype=np.float32)
+    Wg = wl.round_to_bf16(np.array([1e5, -1e5, 1e20, -1e20, 3e38, -3e38], dtype=np.float32)[:, None])
+    Wu = np.full((6, 1), 0.5, dtype=np.float32)
+    H, Z = run_forward(X, Wg, Wu, None, None, kind, "bf16")
+    on = (Wg[:, 0] > 0).astype(np.float64)
+    for n in range(2):
+        within(Z.host()[0][n], 0.5 * on, 0.5 * on * 4 * U32, "Z[0]")
+        within(Z.host()[1][n], np.where(on, lo.f64(Wg[:, 0]), 0.0), np.abs(Wg[:, 0]) * on * 4 * U32, "Z[1]")
+        within(H.host()[n], np.where(on, 0.5 * lo.f64(Wg[:, 0]), 0.0), np.abs(Wg[:, 0]) * on * HALF["bf16"], "H")
+
+
 # -------------------------------------------------------------------------------------------------------- 8-bit product
 
 INT8_SIZES = [(1, 1, 1), (1, 16, 5), (1, 4608, 100), (2, 33, 65), (3, 130, 64), (7, 1000, 200), (16, 576, 96), (17, 72, 257), (32, 512, 512), (33, 48, 130),
