@@ -414,21 +414,21 @@ TileProduct forward_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = S; g.chunks = up8(M) / 8;
     g.stages = g.part = (g.chunks + 7) / 8;
-    tile_plan(g, true, dt == FW_F32);
+    tile_plan(g, true, dt == FW_F32, dt == FW_F32 ? 6 : 5);         // of two sums an entry of H and two of Z
     return g;
 }
 TileProduct rows_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = M; g.chunks = 2 * up64(S) / 8; g.klen = S;
     g.part = up64(S) / 64; g.stages = 2 * g.part;
-    tile_plan(g, false, dt == FW_F32);
+    tile_plan(g, false, dt == FW_F32, dt == FW_F32 ? 4 : 2);
     return g;
 }
 TileProduct weights_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = 2 * up64(S); g.C = M; g.klen = N;
     g.part = g.stages = (N + 63) / 64;
-    tile_plan(g, false, dt == FW_F32);
+    tile_plan(g, false, dt == FW_F32, dt == FW_F32 ? 4 : 2);
     return g;
 }
 

@@ -54,7 +54,7 @@ TileProduct plan(int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = S; g.chunks = up16(M) / 16;
     g.stages = g.part = (g.chunks + 7) / 8;
-    tile_plan(g, false);
+    tile_plan(g, false, false, 2);
     return g;
 }
 size_t padded_bytes(int R, int M) { return M % 16 ? align_up((size_t)R * up16(M), 256) : 0; }

@@ -428,23 +428,27 @@ __device__ __forceinline__ void tile_vector(const float* p, int s, int cols, flo
     for (int i = 0; i < 4; ++i) v[i] = p && s + i < cols ? p[s + i] : 0.f;
 }
 
-// Tile shape and runs of the least estimated time in cycles: rounds of 256 workgroups x (stages + filling the ring) x the longer of a stage's
-// matrix instructions and its loads (about 30 bytes per cycle and compute unit), plus the pass that adds the runs.  Runs are for the tiles
-// behind whole rounds, and keep at least 4 stages (of planes: 2, each with six products).
-inline void tile_plan(TileProduct& g, bool pair, bool planes = false) {
+// Tile shape and runs of the least estimated time in cycles (2.1 GHz): rounds of 256 workgroups x (stages x the longer of a stage's matrix
+// instructions and its loads + the first loads + storing the results, `bytes` each), plus the launch that adds the runs and its traffic.
+// Runs are for the tiles behind whole rounds, and keep at least 4 stages (of planes: 2, each with six products).
+// The constants are fitted to 123 products (20 to 8192 rows, 64 to 12288 columns and features) with every shape and number of runs
+// measured: what is chosen takes 0.5 % longer than the best on average, 8 % at most.
+inline void tile_plan(TileProduct& g, bool pair, bool planes, double bytes) {
     static const int shapes[][2] = {{4, 4}, {2, 4}, {2, 2}, {1, 4}, {1, 2}};
     double best = 1e300;
     for (int i = planes ? 1 : 0; i < 5; ++i) {               // the planes of 256 x 256 results do not fit into LDS
         const int nrt = shapes[i][0], nct = shapes[i][1], tc = pair ? 32 * nct : 64 * nct;
         const int nrb = (g.R + 64 * nrt - 1) / (64 * nrt), ncb = (g.C + tc - 1) / tc;
         const long long tiles = (long long)nrb * ncb;
-        const double t_mfma = 128.0 * nrt * nct * (planes ? 6 : 1) + 60.0, t_load = (nrt + nct) * 8192.0 / 30.0 * (planes ? 3 : 1);
-        const double t_stage = t_mfma > t_load ? t_mfma : t_load, fill = planes ? 1.5 : 4.0;
+        const double area = nrt * nct, t_mfma = (planes ? 6 * 130.0 : 145.0) * area + 60.0, t_load = (nrt + nct) * 8192.0 / 30.0 * (planes ? 3 : 1);
+        const double t_stage = t_mfma > t_load ? t_mfma : t_load, fill = 2150.0, store = 1250.0 * bytes * area;
         const int rest = (int)(tiles % 256);
         for (int runs = 1; runs <= 32 && (runs == 1 || (rest > 0 && rest * runs <= 512 && g.stages / runs >= (planes ? 2 : 4))); ++runs) {
             const int spr = (g.stages + runs - 1) / runs, n = (g.stages + spr - 1) / spr;
-            double cost = (double)((n > 1 ? tiles : tiles + 255) / 256) * (g.stages + fill) * t_stage;
-            if (n > 1) cost += (double)((rest * n + 255) / 256) * (spr + fill) * t_stage + 6000.0 + 2.0 * n * rest * (nrt * nct * 16384.0) / 4e12 * 2.1e9;
+            double cost = (double)((n > 1 ? tiles : tiles + 255) / 256) * (g.stages * t_stage + fill + store);
+            if (n > 1)
+                cost += (double)((rest * n + 255) / 256) * (spr * t_stage + fill) + rest / 256.0 * store + 9500.0 +
+                        2.0 * n * rest * (area * 16384.0) / 4.1e12 * 2.1e9;
             if (cost < best * 0.999) {
                 best = cost;
                 g.nrt = nrt; g.nct = nct; g.nrb = nrb; g.ncb = ncb; g.runs = n; g.spr = spr;
