@@ -358,7 +358,8 @@ fw_status fw_cond_probe(const float* Phi_y, int M, const float* b0, int k, float
 /* ------------------------------------------------------------------------------------------------------------
  * (5) Layers of a language model around the whitening: what makes a layer's input rows X [N, M] (one row per token, the rows that
  * fw_cov_accumulate takes as FW_LAYOUT_ROWS), its products, its weight gradients G [S, M], and its answers in 8 bits.  N, M and S
- * need not be multiples of anything.  Limits of all of them: N <= 2097152, M <= 32768,
+ * need not be multiples of anything; the products copy their operands once to aligned rows where M is not a multiple of 8 (bfloat16)
+ * or 16 (8 bits) and there are more than 16 rows.  Limits of all of them: N <= 2097152, M <= 32768,
  * S <= 65536.  The workspaces are asked for with
  * d = {N, M, 1, 1, 1, 1, 1, 0, 0}, the geometry of N rows.
  *
@@ -427,8 +428,11 @@ fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, cons
  *   dWg, dWu    out  [S, M] element type `dt`, or both NULL
  *   dbg, dbu    out  [S] element type `dt`, or both NULL
  *   ws          scratch, fw_workspace_bytes(FW_OP_GATED_GRAD, M, S, d, dt) bytes
- * FW_BF16: dg and du are rounded to bfloat16 for the products (and for mu's part in them), the sums are float32 and each result is
- * rounded once; dbg and dbu are sums of the values before that rounding.
+ * FW_BF16: dg and du are rounded to bfloat16 for the products (and for mu's part in them) where N S > 524288, below they are held as two
+ * bfloat16 numbers each (the rounding would not average out); the sums are float32 and each result is rounded once; dbg and dbu are
+ * sums of the values before that rounding.
+ * FW_F32: float32 accuracy as in fw_grad_transform's products of three bfloat16 numbers; entries below 2^-110 lose their last bits.  An
+ * infinite or NaN entry reaches the results that the formula lets it reach; those are computed one by one, slowly.
  */
 fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* Z,
                         const void* dH, const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws,

@@ -4,7 +4,7 @@
 //
 // bfloat16: both projections in one launch, the panel of weights holding the same columns of Wg and Wu, so that a lane has g and u of
 // an element in its registers when the sums are done (tile_product.h).  The backward pass forms D = [dg | du] once, rounded to
-// bfloat16, [N][2 Sp] with Sp = S rounded up to 64 and zeros between, and takes two products of it: dX = D [Wg; Wu], whose contraction runs
+// bfloat16 (small N S: to two bfloat16 numbers, see two_planes), [N][2 Sp] with Sp = S rounded up to 64 and zeros between, and takes two products of it: dX = D [Wg; Wu], whose contraction runs
 // over the rows of both weight matrices, and [dWg; dWu] = D^T X.  Operands that are contraction-major in memory are turned on the
 // way out of LDS, not in memory.  mu is taken out of the sums: D^T (X - 1 mu^T) = D^T X - (D^T 1) mu^T, with D^T 1 summed from the
 // rounded D, so that the identity is exact but for float32 sums.
@@ -46,7 +46,8 @@ template <class F> __device__ __forceinline__ void with_activation(int act, cons
     else f(std::integral_constant<int, FW_ACT_RELU>());
 }
 
-// ---- epilogues: four entries of a row.  FIX (float32 planes): entries that are not finite are computed once more.
+// ---- epilogues: four entries of a row.  FIX (operands in planes: an infinite number has none): entries that are not finite are computed
+// once more, in float32.
 __device__ __forceinline__ bool all_finite(const floatx4& v) {
     return fabsf(v[0]) <= 3.402823466e38f && fabsf(v[1]) <= 3.402823466e38f && fabsf(v[2]) <= 3.402823466e38f && fabsf(v[3]) <= 3.402823466e38f;
 }
@@ -91,19 +92,18 @@ template <class T> struct GateEpilogue {
         }
     }
 };
-// what the float32 gradients are computed from once more
-struct GradInputs { const float *X, *Wg, *Wu, *Z, *dH, *mu; int N, M, S; };
-template <class T> struct RowsEpilogue {                     // dX
-    static constexpr bool FIX = std::is_same<T, float>::value;
+// what the gradients are computed from once more
+template <class T> struct GradInputs { const T *X, *Wg, *Wu; const float* Z; const T* dH; const float* mu; int N, M, S; };
+template <class T, bool FIX> struct RowsEpilogue {           // dX
     T* out;
     int N, M;
-    GradInputs in;
+    GradInputs<T> in;
     __device__ __noinline__ float dot(int n, int m) const {
         float v = 0.f;
         for (int s = 0; s < in.S; ++s) {
             const size_t e = (size_t)n * in.S + s, w = (size_t)s * M + m;
-            v = fmaf(in.dH[e] * in.Z[e], in.Wg[w], v);
-            v = fmaf(in.dH[e] * in.Z[(size_t)N * in.S + e], in.Wu[w], v);
+            v = fmaf((float)in.dH[e] * in.Z[e], (float)in.Wg[w], v);
+            v = fmaf((float)in.dH[e] * in.Z[(size_t)N * in.S + e], (float)in.Wu[w], v);
         }
         return v;
     }
@@ -115,28 +115,28 @@ template <class T> struct RowsEpilogue {                     // dX
         tile_store(out + (size_t)n * M + m, m, M, v);
     }
 };
-template <class T> struct WeightsEpilogue {                  // rows below Sp are the gate's, the others the up projection's
-    static constexpr bool FIX = std::is_same<T, float>::value;
+template <class T, bool FIX> struct WeightsEpilogue {        // rows below Sp are the gate's, the others the up projection's
     T *dWg, *dWu;
     const float *sums, *mu;               // mu: taken out here (bfloat16), or null
     int S, Sp, M;
-    GradInputs in;
+    GradInputs<T> in;
     __device__ __noinline__ float dot(int s, bool up, int m) const {
         const float c = in.mu ? in.mu[m] : 0.f;
         float v = 0.f;
         for (int n = 0; n < in.N; ++n) {
             const size_t e = (size_t)n * S + s;
-            v = fmaf(in.dH[e] * in.Z[(up ? (size_t)in.N * S : 0) + e], in.X[(size_t)n * M + m] - c, v);
+            v = fmaf((float)in.dH[e] * in.Z[(up ? (size_t)in.N * S : 0) + e], (float)in.X[(size_t)n * M + m] - c, v);
         }
         return v;
     }
     __device__ __forceinline__ void apply(int r, int m, floatx4 acc) const {
         const int s = r >= Sp ? r - Sp : r;
         if (s >= S || m >= M) return;
-        if (FIX && !all_finite(acc))
+        const bool again = FIX && !all_finite(acc);
+        if (again)
             for (int i = 0; i < 4 && m + i < M; ++i) acc[i] = dot(s, r >= Sp, m + i);
         float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-        if (mu) {
+        if (mu && !again) {
             const float d = sums[r];
             float c[4];
             tile_vector(mu, m, M, c);
@@ -247,17 +247,16 @@ __device__ __forceinline__ void load4(const __bf16* p, float (&x)[4]) {
     for (int i = 0; i < 4; ++i) x[i] = (float)v[i];
 }
 __device__ __forceinline__ void load4(const float* p, float (&x)[4]) { __builtin_memcpy(x, p, 16); }
-// D[n] = [dg | du] of row n, each Sp wide (zeros past S), float32 as three planes [3][Np][2 Sp] (zeros past N).  A workgroup has 256 columns
+// D[n] = [dg | du] of row n, each Sp wide (zeros past S), as P planes [P][Np][2 Sp] (float32: three, zeros past N).  A workgroup has 256 columns
 // and `rows` rows, a wavefront a quarter of these, four at a time (their loads go out together).
 // part[block of rows][4][Sp] or null: sums over the block's rows of dg and du as they are (for the biases) and as rounded (for mu).
-template <class T>
+template <class T, int P>
 __global__ __launch_bounds__(256) void gate_grad_kernel(const T* __restrict__ dH, const float* __restrict__ Z, int N, int Np, int S, int Sp,
                                                         int rows, __bf16* __restrict__ D, float* __restrict__ part) {
-    constexpr bool planes = std::is_same<T, float>::value;
     __shared__ float red[4][4][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int s = blockIdx.x * 256 + 4 * lane;
-    const int n0 = blockIdx.y * rows + wave * (rows / 4), end = planes ? Np : N, n1 = min(n0 + rows / 4, end);
+    const int n0 = blockIdx.y * rows + wave * (rows / 4), end = P == 3 ? Np : N, n1 = min(n0 + rows / 4, end);
     float sum[4][4] = {};
     auto put = [&](__bf16* d, const float (&x)[4], float (&exact)[4], float (&rounded)[4]) __attribute__((always_inline)) {
         bf16x4 h, m, l;
@@ -267,14 +266,12 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(const T* __restrict__ dH
             planes_of(x[i], a, b, c);
             h[i] = a; m[i] = b; l[i] = c;
             exact[i] += x[i];
-            rounded[i] += (float)a;
+            rounded[i] += P == 2 ? (float)a + (float)b : (float)a;
         }
         *reinterpret_cast<bf16x4*>(d) = h;
-        if (planes) {
-            const size_t plane = (size_t)Np * 2 * Sp;
-            *reinterpret_cast<bf16x4*>(d + plane) = m;
-            *reinterpret_cast<bf16x4*>(d + 2 * plane) = l;
-        }
+        const size_t plane = (size_t)Np * 2 * Sp;
+        if (P > 1) *reinterpret_cast<bf16x4*>(d + plane) = m;
+        if (P > 2) *reinterpret_cast<bf16x4*>(d + 2 * plane) = l;
     };
     auto rows_at = [&](auto WHOLE, int n) __attribute__((always_inline)) {       // WHOLE: four columns and four rows, all there
         float h[4][4], p[4][4], q[4][4];
@@ -369,6 +366,10 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(Pad s, int M, int Mp) {
 inline unsigned blocks_for(size_t n) { return (unsigned)((n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384); }
 inline int up8(int m) { return (m + 7) / 8 * 8; }
 inline int up64(int s) { return (s + 63) / 64 * 64; }
+// bfloat16: D in two planes, 16 bits, where the rounding to 8 bits does not average out: it adds an error as large as that of rounding the
+// result, 1.42 times the latter together, but up to 1.8 times where a few entries make up the sum (11 x 64, S = 64).  The products then
+// go over the weights twice; small ones are bound by their launches.
+inline bool two_planes(fw_dtype dt, int N, int S) { return dt == FW_BF16 && (long long)N * S <= 1 << 19; }
 // rows of a workgroup of gate_grad_kernel: 64, or 16 where that leaves compute units without work (777 x 1001: 13.9 us with 64)
 inline int grad_rows(int N, int S) { return (long long)((N + 63) / 64) * ((S + 255) / 256) >= 1024 ? 64 : 16; }
 inline int row_blocks(int N, int S) { return (up64(N) + grad_rows(N, S) - 1) / grad_rows(N, S); }
@@ -413,21 +414,21 @@ struct Carve {
 TileProduct forward_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = S; g.chunks = up8(M) / 8;
-    g.stages = g.part = (g.chunks + 7) / 8;
+    g.stages = g.once = g.part = (g.chunks + 7) / 8;
     tile_plan(g, true, dt == FW_F32, dt == FW_F32 ? 6 : 5);         // of two sums an entry of H and two of Z
     return g;
 }
 TileProduct rows_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = M; g.chunks = 2 * up64(S) / 8; g.klen = S;
-    g.part = up64(S) / 64; g.stages = 2 * g.part;
+    g.part = up64(S) / 64; g.once = 2 * g.part; g.stages = two_planes(dt, N, S) ? 2 * g.once : g.once;
     tile_plan(g, false, dt == FW_F32, dt == FW_F32 ? 4 : 2);
     return g;
 }
 TileProduct weights_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = 2 * up64(S); g.C = M; g.klen = N;
-    g.part = g.stages = (N + 63) / 64;
+    g.part = g.once = (N + 63) / 64; g.stages = two_planes(dt, N, S) ? 2 * g.once : g.once;
     tile_plan(g, false, dt == FW_F32, dt == FW_F32 ? 4 : 2);
     return g;
 }
@@ -457,7 +458,7 @@ GradWs grad_ws(fw_dtype dt, int N, int M, int S, void* ws) {
     Carve c = {reinterpret_cast<char*>(ws)};
     GradWs w = {};
     const size_t Sp = up64(S);
-    w.D = c.take(dt == FW_F32 ? plane3_bytes(up64(N), 2 * (int)Sp) : (size_t)N * 2 * Sp * 2);
+    w.D = c.take(dt == FW_F32 ? plane3_bytes(up64(N), 2 * (int)Sp) : (size_t)N * 2 * Sp * (two_planes(dt, N, S) ? 4 : 2));
     w.part = reinterpret_cast<float*>(c.take((size_t)row_blocks(N, S) * 4 * Sp * 4));
     w.sums = reinterpret_cast<float*>(c.take(2 * Sp * 4));
     if (dt == FW_F32) {
@@ -526,8 +527,13 @@ template <class T>
 fw_status gate_grad(const T* dH, const float* Z, int N, int S, const GradWs& w, bool rounded, T* dbg, T* dbu, hipStream_t st) {
     const int Sp = up64(S);
     const bool sums = rounded || dbg;
-    hipLaunchKernelGGL(gate_grad_kernel<T>, dim3((Sp + 255) / 256, row_blocks(N, S)), dim3(256), 0, st, dH, Z, N, up64(N), S, Sp,
-                       grad_rows(N, S), reinterpret_cast<__bf16*>(w.D), sums ? w.part : nullptr);
+    const auto launch = [&](auto P) {
+        hipLaunchKernelGGL((gate_grad_kernel<T, decltype(P)::value>), dim3((Sp + 255) / 256, row_blocks(N, S)), dim3(256), 0, st, dH, Z, N,
+                           decltype(P)::value == 3 ? up64(N) : N, S, Sp, grad_rows(N, S), reinterpret_cast<__bf16*>(w.D), sums ? w.part : nullptr);
+    };
+    if constexpr (std::is_same<T, float>::value) launch(std::integral_constant<int, 3>());
+    else if (two_planes(FW_BF16, N, S)) launch(std::integral_constant<int, 2>());
+    else launch(std::integral_constant<int, 1>());
     FW_LAUNCH_CHECK();
     if (!sums) return FW_OK;
     hipLaunchKernelGGL(bias_grad_kernel<T>, dim3((rounded ? 4 : 2) * Sp / 64), dim3(1024), 0, st, w.part, row_blocks(N, S), S, Sp, w.sums, dbg, dbu);
@@ -541,7 +547,7 @@ fw_status grad_f32(const float* X, int N, int M, int S, const float* Wg, const f
     const int Sp = up64(S), Np = up64(N);
     fw_status rc = gate_grad<float>(dH, Z, N, S, w, false, dbg, dbu, st);
     if (rc != FW_OK) return rc;
-    const GradInputs in = {X, Wg, Wu, Z, dH, mu, N, M, S};
+    const GradInputs<float> in = {X, Wg, Wu, Z, dH, mu, N, M, S};
     Split s = {};
     int k = 0;
     const auto add = [&](const float* p, void* out, int R, int Rp, const float* c) { s.in[k] = p; s.out[k] = (__bf16*)out; s.R[k] = R; s.Rp[k] = Rp; s.mu[k++] = c; };
@@ -555,7 +561,7 @@ fw_status grad_f32(const float* X, int N, int M, int S, const float* Wg, const f
         g.apitch = 4ll * Sp; g.bpitch = 2ll * up64(M);
         g.aplane = Np * g.apitch; g.bplane = Sp * g.bpitch;
         g.partial = w.partial;
-        rc = tile_product<TILE_PLANES, false, true, false>(g, RowsEpilogue<float>{dX, N, M, in}, st);
+        rc = tile_product<TILE_PLANES, false, true, false>(g, RowsEpilogue<float, true>{dX, N, M, in}, st);
         if (rc != FW_OK) return rc;
     }
     if (dWg) {
@@ -564,7 +570,7 @@ fw_status grad_f32(const float* X, int N, int M, int S, const float* Wg, const f
         g.apitch = 4ll * Sp; g.bpitch = 2ll * up64(M);
         g.aplane = Np * g.apitch; g.bplane = Np * g.bpitch;
         g.partial = w.partial;
-        rc = tile_product<TILE_PLANES, true, true, false>(g, WeightsEpilogue<float>{dWg, dWu, nullptr, nullptr, S, Sp, M, in}, st);
+        rc = tile_product<TILE_PLANES, true, true, false>(g, WeightsEpilogue<float, true>{dWg, dWu, nullptr, nullptr, S, Sp, M, in}, st);
     }
     return rc;
 }
@@ -573,6 +579,8 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
                     __bf16* dX, __bf16* dWg, __bf16* dWu, __bf16* dbg, __bf16* dbu, void* ws, hipStream_t st) {
     const GradWs w = grad_ws(FW_BF16, N, M, S, ws);
     const int Sp = up64(S);
+    const bool two = two_planes(FW_BF16, N, S);
+    const GradInputs<__bf16> in = {(const __bf16*)X, (const __bf16*)Wg, (const __bf16*)Wu, Z, dH, mu, N, M, S};       // as they came, not padded
     fw_status rc = gate_grad<__bf16>(dH, Z, N, S, w, mu && dWg, dbg, dbu, st);
     if (rc != FW_OK) return rc;
     if (M % 8) {
@@ -586,17 +594,19 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
     if (dX) {
         TileProduct g = rows_plan(FW_BF16, N, M, S);
         g.a = bytes(w.D); g.b0 = bytes(Wg); g.b1 = bytes(Wu);
-        g.apitch = 4ll * Sp; g.bpitch = 2ll * up8(M);
+        g.apitch = 4ll * Sp; g.bpitch = 2ll * up8(M); g.aplane = N * g.apitch;
         g.partial = w.partial;
-        rc = tile_product<TILE_BF16, false, true, false>(g, RowsEpilogue<__bf16>{dX, N, M, {}}, st);
+        rc = two ? tile_product<TILE_BF16, false, true, false>(g, RowsEpilogue<__bf16, true>{dX, N, M, in}, st)
+                 : tile_product<TILE_BF16, false, true, false>(g, RowsEpilogue<__bf16, false>{dX, N, M, in}, st);
         if (rc != FW_OK) return rc;
     }
     if (dWg) {
         TileProduct g = weights_plan(FW_BF16, N, M, S);
         g.a = bytes(w.D); g.b0 = g.b1 = bytes(X);
-        g.apitch = 4ll * Sp; g.bpitch = 2ll * up8(M);
+        g.apitch = 4ll * Sp; g.bpitch = 2ll * up8(M); g.aplane = N * g.apitch;
         g.partial = w.partial;
-        rc = tile_product<TILE_BF16, true, true, false>(g, WeightsEpilogue<__bf16>{dWg, dWu, w.sums, mu, S, Sp, M, {}}, st);
+        rc = two ? tile_product<TILE_BF16, true, true, false>(g, WeightsEpilogue<__bf16, true>{dWg, dWu, w.sums, mu, S, Sp, M, in}, st)
+                 : tile_product<TILE_BF16, true, true, false>(g, WeightsEpilogue<__bf16, false>{dWg, dWu, w.sums, mu, S, Sp, M, in}, st);
     }
     return rc;
 }

@@ -53,7 +53,7 @@ fw_status pad_bytes(const signed char* in, int R, int M, void* out, hipStream_t 
 TileProduct plan(int N, int M, int S) {
     TileProduct g = {};
     g.R = N; g.C = S; g.chunks = up16(M) / 16;
-    g.stages = g.part = (g.chunks + 7) / 8;
+    g.stages = g.once = g.part = (g.chunks + 7) / 8;
     tile_plan(g, false, false, 2);
     return g;
 }

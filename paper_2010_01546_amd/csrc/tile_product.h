@@ -23,6 +23,7 @@
 //   as a product of its own, each with its loads: 1024 x 576 x 2304, 61 us forward; loads bound it.)  The planes are padded with zeros to
 //   whole stages.  Entries below 2^-110 lose their last bits (bfloat16 ends at 2^-133); where a result is not finite (an infinite entry
 //   has no such sum) the epilogue computes it once more in float32.
+// Two operands A may meet the same B one after the other (once): sums of a product whose A is the sum of two bfloat16 numbers.
 // Where the contraction ends inside a stage, the loads past the end fetch a zero (in both operands: 0 x NaN is NaN).  Rows or columns past
 // the edge are clamped; they feed results that the epilogue does not store.
 //
@@ -47,8 +48,8 @@ struct TileProduct {
     int R, C;                     // results; PAIR: C columns of each matrix
     int chunks;                   // 16-byte chunks of a row (operands along the contraction)
     int klen;                     // k of a part (contraction-major operands)
-    int part, stages;             // stages of the first part, stages in all
-    long long aplane, bplane;     // TILE_PLANES: bytes between planes
+    int part, once, stages;       // stages of a part, of one pass over B, in all
+    long long aplane, bplane;     // TILE_PLANES: bytes between planes; once < stages: aplane to the second operand that meets B again
     int nrb, ncb;                 // rows and columns of tiles
     int full, rest;               // tiles with the whole contraction, tiles cut into runs (none where runs is 1)
     int runs, spr;                // runs, stages of a run
@@ -182,13 +183,15 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     const long long second = BKM ? g.b1 - g.b0 : 0;
     // stages that lie inside the contraction with all their chunks (of a part)
     const int whole = AKM || BKM ? g.klen >> 6 : g.chunks >> 3;
-    struct Stage { const char *a, *b; int c, cb; };
+    struct Stage { const char *a, *b; int c, ca, cb; };         // stage, and within a pass over B and a part
     auto stage_at = [&](int c) __attribute__((always_inline)) {
         Stage s;
         s.c = c;
-        const bool two = BKM && c >= g.part;
-        s.cb = two ? c - g.part : c;
-        s.a = base_a + (AKM ? (long long)c * 64 * g.apitch : (long long)c * 128);
+        const bool again = BKM && KIND == TILE_BF16 && c >= g.once;
+        s.ca = again ? c - g.once : c;
+        const bool two = BKM && s.ca >= g.part;
+        s.cb = two ? s.ca - g.part : s.ca;
+        s.a = base_a + (AKM ? (long long)s.ca * 64 * g.apitch : (long long)s.ca * 128) + (again ? g.aplane : 0);
         s.b = base_b + (BKM ? (long long)s.cb * 64 * g.bpitch + (two ? second : 0) : (long long)c * 128);
         return s;
     };
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
         if constexpr (decltype(ALL)::value) {
             dma16_from(isa ? s.a : s.b, vof[k], to);
         } else {
-            const int c = isa ? s.c : s.cb, RP = 8 / (isa ? NRT : NCT);
+            const int c = isa ? s.ca : s.cb, RP = 8 / (isa ? NRT : NCT);
             const bool major = isa ? AKM : BKM;
             const bool inside = s.c < cend && (major ? 64 * c + (wave + NW * (isa ? k : k - LA)) * RP + lane / (64 / RP) < g.klen
                                                      : 8 * c + chunk < g.chunks);
@@ -285,7 +288,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
 #pragma unroll
         for (int f = 0; f < NF; ++f) read_one(at_a, B0 + at_b, 0, f);
         int a0 = 0, b0 = B0;                         // the stage's buffers
-        int c = c0;
+        int c = c0, begun = 0;                       // the part that stage c + D lies in
         auto turn = [&](auto ALL) __attribute__((always_inline)) {
             const int a1 = a0 == D * Shape::PA ? 0 : a0 + Shape::PA, free_a = a0 == 0 ? D * Shape::PA : a0 - Shape::PA;
             const int b1 = b0 == BE - Shape::PB ? B0 : b0 + Shape::PB;
@@ -301,7 +304,8 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
         };
         while (c < cend) {
             // stages up to `fast` ask for whole ones only
-            const int fast = min(cend, BKM && c + D >= g.part ? g.part + whole : min(whole, g.part)) - D;
+            while (BKM && c + D >= begun + g.part) begun += g.part;
+            const int fast = min(cend, begun + min(whole, g.part)) - D;
             while (c < fast) turn(std::true_type());
             turn(std::false_type());
         }
