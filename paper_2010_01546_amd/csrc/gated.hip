@@ -10,7 +10,7 @@
 // rounded D, so that the identity is exact but for float32 sums.
 // float32: the same products with every operand as three bfloat16 planes (tile_product.h), split in one pass over X and the weights, D
 // when it is formed.  X is centred on mu as it is split.
-// float32 with few rows: the weights are read once as they are, each by one wavefront (few_rows_kernel).
+// float32 with few rows: float32 matrix instructions on the operands as they are (few_product_kernel), one row without them.
 #include "fw_internal.h"
 #include "tile_product.h"
 
@@ -51,8 +51,7 @@ template <class F> __device__ __forceinline__ void with_activation(int act, cons
 __device__ __forceinline__ bool all_finite(const floatx4& v) {
     return fabsf(v[0]) <= 3.402823466e38f && fabsf(v[1]) <= 3.402823466e38f && fabsf(v[2]) <= 3.402823466e38f && fabsf(v[3]) <= 3.402823466e38f;
 }
-template <class T> struct GateEpilogue {
-    static constexpr bool FIX = std::is_same<T, float>::value;
+template <class T, bool FIX> struct GateEpilogue {
     T* H;
     float* Z;
     const float *bg, *bu;
@@ -147,58 +146,40 @@ template <class T, bool FIX> struct WeightsEpilogue {        // rows below Sp ar
     }
 };
 
-// ---- elementwise passes
-// float32, up to FEW rows: a wavefront takes the two weight rows of an output, NR rows of X at a time (from the caches: all wavefronts read
-// the same ones).
-constexpr int FEW = 16;
-template <int NR>
-__global__ __launch_bounds__(256) void few_rows_kernel(const float* __restrict__ X, int N, int M, int S, const float* __restrict__ Wg,
-                                                       const float* __restrict__ Wu, GateEpilogue<float> epi) {
-    const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6), n0 = blockIdx.y * NR;
+// float32, one row: a wavefront takes the two weight rows of an output.  Bound by the one read of the weights (4172
+// features to 7040: 48.0 us, 4.9 TB/s; on the matrix cores as for more rows 55.6).
+__global__ __launch_bounds__(256) void one_row_kernel(const float* __restrict__ X, int M, int S, const float* __restrict__ Wg,
+                                                      const float* __restrict__ Wu, GateEpilogue<float, false> epi) {
+    const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (s >= S) return;
     const float *wg = Wg + (size_t)s * M, *wu = Wu + (size_t)s * M;
-    float g[NR], u[NR];
-#pragma unroll
-    for (int r = 0; r < NR; ++r) g[r] = u[r] = 0.f;
+    float g = 0.f, u = 0.f;
     const int whole = M / 256 * 256;
 #pragma unroll 2
     for (int m = 4 * lane; m < whole; m += 256) {
-        float4 a, b;
+        float4 a, b, x;
         __builtin_memcpy(&a, wg + m, 16);
         __builtin_memcpy(&b, wu + m, 16);
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            float4 x;
-            __builtin_memcpy(&x, X + (size_t)min(n0 + r, N - 1) * M + m, 16);
-            g[r] = fmaf(x.x, a.x, fmaf(x.y, a.y, fmaf(x.z, a.z, fmaf(x.w, a.w, g[r]))));
-            u[r] = fmaf(x.x, b.x, fmaf(x.y, b.y, fmaf(x.z, b.z, fmaf(x.w, b.w, u[r]))));
-        }
+        __builtin_memcpy(&x, X + m, 16);
+        g = fmaf(x.x, a.x, fmaf(x.y, a.y, fmaf(x.z, a.z, fmaf(x.w, a.w, g))));
+        u = fmaf(x.x, b.x, fmaf(x.y, b.y, fmaf(x.z, b.z, fmaf(x.w, b.w, u))));
     }
     for (int m = whole + lane; m < M; m += 64) {
-        const float a = wg[m], b = wu[m];
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            const float x = X[(size_t)min(n0 + r, N - 1) * M + m];
-            g[r] = fmaf(x, a, g[r]);
-            u[r] = fmaf(x, b, u[r]);
-        }
+        g = fmaf(X[m], wg[m], g);
+        u = fmaf(X[m], wu[m], u);
     }
-#pragma unroll
-    for (int r = 0; r < NR; ++r) { g[r] = wave_sum(g[r]); u[r] = wave_sum(u[r]); }
+    g = wave_sum(g); u = wave_sum(u);
     if (lane) return;
     with_activation(epi.act, [&](auto ACT) {
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            if (n0 + r >= N) break;
-            const float gv = g[r] + (epi.bg ? epi.bg[s] : 0.f), uv = u[r] + (epi.bu ? epi.bu[s] : 0.f);
-            float a, da;
-            activation<decltype(ACT)::value>(gv, a, da);
-            const size_t e = (size_t)(n0 + r) * S + s;
-            epi.H[e] = a * uv;
-            if (epi.Z) { epi.Z[e] = uv * da; epi.Z[(size_t)N * S + e] = a; }
-        }
+        float a, da;
+        activation<decltype(ACT)::value>(g + (epi.bg ? epi.bg[s] : 0.f), a, da);
+        u += epi.bu ? epi.bu[s] : 0.f;
+        epi.H[s] = a * u;
+        if (epi.Z) { epi.Z[s] = u * da; epi.Z[(size_t)S + s] = a; }
     });
 }
+
+// ---- elementwise passes
 
 // three bfloat16 planes of a float32 number
 __device__ __forceinline__ void planes_of(float x, __bf16& h, __bf16& m, __bf16& l) {
@@ -363,6 +344,10 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(Pad s, int M, int Mp) {
     }
 }
 
+// Up to 64 rows float32 products are bound by the one read of the weights or nearly so; in planes these are written and read again (4172
+// features to 7040, 17 rows: 202 us against 68.6, 64 rows: 204 against 118, 86 rows: 215 against 200, 128 rows of 1153 to 1001: 27 against 37).
+constexpr int FEW_F32 = 64;
+
 inline unsigned blocks_for(size_t n) { return (unsigned)((n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384); }
 inline int up8(int m) { return (m + 7) / 8 * 8; }
 inline int up64(int s) { return (s + 63) / 64 * 64; }
@@ -439,7 +424,7 @@ ForwardWs forward_ws(fw_dtype dt, int N, int M, int S, void* ws) {
     Carve c = {reinterpret_cast<char*>(ws)};
     ForwardWs w = {};
     if (dt == FW_F32) {
-        if (N > FEW) {
+        if (N > FEW_F32) {
             w.X = c.take(plane3_bytes(N, M));
             w.Wg = c.take(plane3_bytes(S, M));
             w.Wu = c.take(plane3_bytes(S, M));
@@ -449,7 +434,7 @@ ForwardWs forward_ws(fw_dtype dt, int N, int M, int S, void* ws) {
         w.Wg = c.take((size_t)S * up8(M) * 2);
         w.Wu = c.take((size_t)S * up8(M) * 2);
     }
-    if (N > (dt == FW_BF16 ? TILE_FEW : FEW)) w.partial = c.take(tile_partial_bytes(forward_plan(dt, N, M, S)));
+    if (N > (dt == FW_BF16 ? TILE_FEW : FEW_F32)) w.partial = c.take(tile_partial_bytes(forward_plan(dt, N, M, S)));
     w.total = c.used;
     return w;
 }
@@ -479,18 +464,17 @@ GradWs grad_ws(fw_dtype dt, int N, int M, int S, void* ws) {
 fw_status forward_f32(const float* X, int N, int M, int S, const float* Wg, const float* Wu, const float* bg, const float* bu, fw_act act,
                       float* H, float* Z, void* ws, hipStream_t st) {
     const ForwardWs w = forward_ws(FW_F32, N, M, S, ws);
-    const GateEpilogue<float> epi = {H, Z, bg, bu, N, S, (int)act, X, Wg, Wu, M};
-    if (N <= FEW) {
-        const auto launch = [&](auto NR) {
-            hipLaunchKernelGGL(few_rows_kernel<decltype(NR)::value>, dim3((S + 3) / 4, (N + decltype(NR)::value - 1) / decltype(NR)::value), dim3(256), 0, st,
-                               X, N, M, S, Wg, Wu, epi);
-        };
-        if (N == 1) launch(std::integral_constant<int, 1>());
-        else if (N <= 4) launch(std::integral_constant<int, 4>());
-        else launch(std::integral_constant<int, 8>());
+    if (N <= FEW_F32) {
+        const GateEpilogue<float, false> epi = {H, Z, bg, bu, N, S, (int)act};
+        const FewProduct few = {bytes(X), bytes(Wg), bytes(Wu), N, S, 4 * M};
+        if (N > 32) return few_product<TILE_F32, true, 4>(few, epi, st);
+        if (N > 16) return few_product<TILE_F32, true, 2>(few, epi, st);
+        if (N > 1) return few_product<TILE_F32, true, 1>(few, epi, st);
+        hipLaunchKernelGGL(one_row_kernel, dim3((S + 3) / 4), dim3(256), 0, st, X, M, S, Wg, Wu, epi);
         FW_LAUNCH_CHECK();
         return FW_OK;
     }
+    const GateEpilogue<float, true> epi = {H, Z, bg, bu, N, S, (int)act, X, Wg, Wu, M};
     const Split s = {{X, Wg, Wu}, {(__bf16*)w.X, (__bf16*)w.Wg, (__bf16*)w.Wu}, {N, S, S}, {N, S, S}, {}};
     const fw_status rc = split_planes(s, 3, M, st);
     if (rc != FW_OK) return rc;
@@ -505,7 +489,7 @@ fw_status forward_f32(const float* X, int N, int M, int S, const float* Wg, cons
 fw_status forward_bf16(const void* X, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu, fw_act act,
                        void* H, float* Z, void* ws, hipStream_t st) {
     const ForwardWs w = forward_ws(FW_BF16, N, M, S, ws);
-    const GateEpilogue<__bf16> epi = {reinterpret_cast<__bf16*>(H), Z, bg, bu, N, S, (int)act};
+    const GateEpilogue<__bf16, false> epi = {reinterpret_cast<__bf16*>(H), Z, bg, bu, N, S, (int)act};
     if (N <= TILE_FEW) return few_product<TILE_BF16, true>({bytes(X), bytes(Wg), bytes(Wu), N, S, 2 * M}, epi, st);
     if (M % 8) {             // 16-byte loads need aligned rows
         PadList pads;

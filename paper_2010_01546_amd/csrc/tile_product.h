@@ -40,7 +40,7 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 
 static __device__ uint4 tile_zero;          // 16 bytes of zeros, never written
 
-enum TileKind { TILE_BF16, TILE_I8, TILE_PLANES };
+enum TileKind { TILE_BF16, TILE_I8, TILE_PLANES, TILE_F32 };      // TILE_F32: few rows alone
 
 struct TileProduct {
     const char *a, *b0, *b1;      // operands; b1: a second matrix, of the same tile's other columns (PAIR) or of the contraction's second part
@@ -486,9 +486,10 @@ fw_status tile_product(const TileProduct& g, const Epi& epi, hipStream_t st) {
     return tile_launch<KIND, 1, 2, 8, AKM, BKM, PAIR>(g, epi, st);
 }
 
-// ---- few rows: C[r][c] = sum_k A[r][k] B[c][k] for up to 16 rows, rows along the contraction and of any length.  Bound by the one read of B.
+// ---- few rows: C[r][c] = sum_k A[r][k] B[c][k] for up to 16 NA rows, rows along the contraction and of any length.  Bound by
+// the one read of B; float32 (products by v_mfma_f32_16x16x4_f32) from about 50 rows on by the matrix instructions.
 // A workgroup owns `cols` columns (PAIR: of each matrix), so many that every compute unit gets as much of B to read; its wavefronts take
-// stages of 128 bytes in turn, two ahead in registers, turn them through 6 KB of LDS of their own (eight lanes load the 128 bytes of a
+// stages of 128 bytes in turn, two ahead in registers, turn them through LDS of their own (eight lanes load the 128 bytes of a
 // row, so that whole cache lines are asked for) and add up their sums at the end: one launch, no workspace, no padded copies.
 // Two projections of one row of 4608 bfloat16, 12288 columns: 42.7 us, 5.3 TB/s; 16 rows of 12288 bytes, 4608 columns: 11.6 us, 4.9 TB/s.
 // (Tiles of 64 rows whose contraction is cut into runs: 43.7 and 18.0 us; 1 x 1153, 1001 columns, whose rows these need padded: 13.3
@@ -498,64 +499,73 @@ struct FewProduct {
     const char *a, *b0, *b1;
     int N, C, bytes, cols;        // rows, columns (PAIR: of each matrix), bytes of a row, columns of a workgroup
 };
-template <TileKind KIND, bool PAIR, class Epi>
-__global__ __launch_bounds__(512, 4) void few_product_kernel(FewProduct g, Epi epi) {
+template <TileKind KIND, int NA, bool PAIR, class Epi>
+__global__ __launch_bounds__(512, NA > 1 ? 2 : 4) void few_product_kernel(FewProduct g, Epi epi) {
     constexpr bool I8 = KIND == TILE_I8;
-    constexpr int NW = 8;
+    constexpr int NW = 8, NV = 4 + 2 * NA;                            // pieces of 8 rows of a stage: 32 rows of B, 16 NA of A
     using Acc = typename std::conditional<I8, intx4, floatx4>::type;
-    __shared__ __align__(16) char lds[NW][6144];                      // a wavefront's stage: 32 rows of B, 16 of A
+    __shared__ __align__(16) char lds[NW][1024 * NV];
     const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col0 = blockIdx.x * g.cols, cend = min(g.C, col0 + g.cols);
     const int chunks = g.bytes / 16, stages = (g.bytes + 127) / 128;       // whole chunks of 16 bytes
-    // 48 rows of a stage, eight at a time: where they begin, behind addresses that are the same for the workgroup
+    // where the rows of a stage begin, behind addresses that are the same for the workgroup
     const char *b0 = g.b0 + (size_t)col0 * g.bytes, *b1 = (PAIR ? g.b1 : g.b0) + (size_t)col0 * g.bytes;
-    unsigned at[6];
+    unsigned at[NV];
 #pragma unroll
-    for (int j = 0; j < 6; ++j) {
+    for (int j = 0; j < NV; ++j) {
         const int r = 8 * j + (lane >> 3);
         at[j] = (unsigned)(j < 4 ? min(PAIR ? r & 15 : r, cend - 1 - col0) : min(r - 32, g.N - 1)) * g.bytes;
     }
     auto base = [&](int j) __attribute__((always_inline)) { return j < 2 ? b0 : j < 4 ? b1 : g.a; };
-    struct Stage { intx4 v[6]; };
+    struct Stage { intx4 v[NV]; };
     auto load = [&](Stage& s, int c) __attribute__((always_inline)) {       // chunks outside of the rows: zeros
         const bool in = c >= 0 && 8 * c + (lane & 7) < chunks;
 #pragma unroll
-        for (int j = 0; j < 6; ++j) __builtin_memcpy(&s.v[j], in ? base(j) + at[j] + 128 * c + 16 * (lane & 7) : reinterpret_cast<const char*>(&tile_zero), 16);
+        for (int j = 0; j < NV; ++j) __builtin_memcpy(&s.v[j], in ? base(j) + at[j] + 128 * c + 16 * (lane & 7) : reinterpret_cast<const char*>(&tile_zero), 16);
     };
     auto load_whole = [&](Stage& s, int c) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < 6; ++j) __builtin_memcpy(&s.v[j], base(j) + 128 * c + (at[j] + 16 * (lane & 7)), 16);
+        for (int j = 0; j < NV; ++j) __builtin_memcpy(&s.v[j], base(j) + 128 * c + (at[j] + 16 * (lane & 7)), 16);
     };
-    Acc acc[2] = {Acc{0, 0, 0, 0}, Acc{0, 0, 0, 0}};
+    Acc acc[NA][2];
+#pragma unroll
+    for (int a = 0; a < NA; ++a) acc[a][0] = acc[a][1] = Acc{0, 0, 0, 0};
     // chunk c of row r at c ^ (r / 2 % 8).  A wavefront's accesses to LDS happen in their order; the fences keep the compiler to it.
     auto use = [&](const Stage& s) __attribute__((always_inline)) {
         FW_COMPILER_FENCE();
 #pragma unroll
-        for (int j = 0; j < 6; ++j)
+        for (int j = 0; j < NV; ++j)
             *reinterpret_cast<intx4*>(&lds[wave][(8 * j + (lane >> 3)) * 128 + 16 * ((lane & 7) ^ ((4 * j + (lane >> 4)) & 7))]) = s.v[j];
         FW_COMPILER_FENCE();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            intx4 fr[3];
+            intx4 fr[2 + NA];
 #pragma unroll
-            for (int f = 0; f < 3; ++f) fr[f] = *reinterpret_cast<const intx4*>(&lds[wave][(16 * f + l16) * 128 + 16 * ((4 * h + q) ^ (l16 >> 1))]);
+            for (int f = 0; f < 2 + NA; ++f) fr[f] = *reinterpret_cast<const intx4*>(&lds[wave][(16 * f + l16) * 128 + 16 * ((4 * h + q) ^ (l16 >> 1))]);
 #pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                if constexpr (I8) acc[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fr[f], fr[2], acc[f], 0, 0, 0);
-                else acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fr[f]), __builtin_bit_cast(bf16x8, fr[2]), acc[f], 0, 0, 0);
+            for (int m = 0; m < 2 * NA; ++m) {
+                const int a = m / 2, f = m % 2;
+                if constexpr (I8) {
+                    acc[a][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fr[f], fr[2 + a], acc[a][f], 0, 0, 0);
+                } else if constexpr (KIND == TILE_BF16) {
+                    acc[a][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fr[f]), __builtin_bit_cast(bf16x8, fr[2 + a]), acc[a][f], 0, 0, 0);
+                } else {                                       // k = 4 q + i, the same for both operands
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        acc[a][f] = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(fr[f][i]), __int_as_float(fr[2 + a][i]), acc[a][f], 0, 0, 0);
+                }
             }
         }
     };
-    // from the end of the rows, whose last stage may not be whole, to their beginning
     Stage s, t;
     int c = stages - 1 - wave, more = c >= 0 ? c / NW - 1 : 0;       // stages behind the first two
     load(s, c);
     if (g.bytes % 16 && wave == 0) {                // the chunk that is not whole
         const int n = 8 * c + (lane & 7) == chunks ? g.bytes - 16 * chunks : 0;
-        constexpr int E = I8 ? 1 : 2;
+        constexpr int E = I8 ? 1 : KIND == TILE_BF16 ? 2 : 4;
 #pragma unroll
-        for (int j = 0; j < 6; ++j) {
+        for (int j = 0; j < NV; ++j) {
             union { char b[16]; intx4 v; } u;
             u.v = s.v[j];
 #pragma unroll
@@ -575,33 +585,38 @@ __global__ __launch_bounds__(512, 4) void few_product_kernel(FewProduct g, Epi e
     if (more == 1) load_whole(s, c);
     use(t);
     if (more == 1) use(s);
-    // the wavefronts' sums, in order
-    FW_COMPILER_FENCE();
+    // the wavefronts' sums, in order, 16 rows at a time
 #pragma unroll
-    for (int f = 0; f < 2; ++f) *reinterpret_cast<Acc*>(&lds[wave][1024 * f + 16 * lane]) = acc[f];
-    __syncthreads();
-    const auto total = [&](int f) __attribute__((always_inline)) {
-        Acc v = *reinterpret_cast<const Acc*>(&lds[0][1024 * f + 16 * lane]);
+    for (int a = 0; a < NA; ++a) {
+        FW_COMPILER_FENCE();
+        if (a) __syncthreads();
 #pragma unroll
-        for (int w = 1; w < NW; ++w) {
-            const Acc x = *reinterpret_cast<const Acc*>(&lds[w][1024 * f + 16 * lane]);
+        for (int f = 0; f < 2; ++f) *reinterpret_cast<Acc*>(&lds[wave][1024 * f + 16 * lane]) = acc[a][f];
+        __syncthreads();
+        const auto total = [&](int f) __attribute__((always_inline)) {
+            Acc v = *reinterpret_cast<const Acc*>(&lds[0][1024 * f + 16 * lane]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += x[i];
+            for (int w = 1; w < NW; ++w) {
+                const Acc x = *reinterpret_cast<const Acc*>(&lds[w][1024 * f + 16 * lane]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += x[i];
+            }
+            return v;
+        };
+        const int n = 16 * a + l16;
+        if constexpr (PAIR) {
+            if (wave == 0 && col0 + 4 * q < cend) epi.apply(n, col0 + 4 * q, total(0), total(1));
+        } else {
+            if (wave < 2 && col0 + 16 * wave + 4 * q < cend) epi.apply(n, col0 + 16 * wave + 4 * q, total(wave));
         }
-        return v;
-    };
-    if constexpr (PAIR) {
-        if (wave == 0 && col0 + 4 * q < cend) epi.apply(l16, col0 + 4 * q, total(0), total(1));
-    } else {
-        if (wave < 2 && col0 + 16 * wave + 4 * q < cend) epi.apply(l16, col0 + 16 * wave + 4 * q, total(wave));
     }
 }
-template <TileKind KIND, bool PAIR, class Epi>
+template <TileKind KIND, bool PAIR, int NA = 1, class Epi>
 fw_status few_product(FewProduct g, const Epi& epi, hipStream_t st) {
     constexpr int MOST = PAIR ? 16 : 32;             // columns a workgroup can take
     const int each = (g.C + 255) / 256, parts = (each + MOST - 1) / MOST;
     g.cols = ((each + parts - 1) / parts + 3) / 4 * 4;
-    hipLaunchKernelGGL((few_product_kernel<KIND, PAIR, Epi>), dim3((g.C + g.cols - 1) / g.cols), dim3(512), 0, st, g, epi);
+    hipLaunchKernelGGL((few_product_kernel<KIND, NA, PAIR, Epi>), dim3((g.C + g.cols - 1) / g.cols), dim3(512), 0, st, g, epi);
     FW_LAUNCH_CHECK();
     return FW_OK;
 }

@@ -302,15 +302,16 @@ FEW_SIZES = [(1, 7, 3), (2, 8, 259), (4, 33, 1), (15, 129, 300), (16, 577, 1030)
              (1, 12289, 20)]
 
 
-@pytest.mark.parametrize("N,M,S", FEW_SIZES)
-def test_gated_few_rows(N, M, S):
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M,S", FEW_SIZES + [(49, 127, 517), (64, 1000, 30)])
+def test_gated_few_rows(N, M, S, dtype):
     kind = act_of(N, M, S)
-    _, X, Wg, Wu, bg, bu = gated_inputs(N, M, S, "bf16", S % 2 == 0)
-    H, Z = run_forward(X, Wg, Wu, bg, bu, kind, "bf16")
-    check_forward(H.host(), Z.host(), X, Wg, Wu, bg, bu, kind, "bf16")
+    _, X, Wg, Wu, bg, bu = gated_inputs(N, M, S, dtype, S % 2 == 0)
+    H, Z = run_forward(X, Wg, Wu, bg, bu, kind, dtype)
+    check_forward(H.host(), Z.host(), X, Wg, Wu, bg, bu, kind, dtype)
     # the last weights of a row in front of entries that are no part of it: an infinite row of the weights reaches its own column alone
     Wg[0] = np.inf
-    H2, _ = run_forward(X, Wg, Wu, bg, bu, kind, "bf16", keep=False)
+    H2, _ = run_forward(X, Wg, Wu, bg, bu, kind, dtype, keep=False)
     assert torch.equal(H2.t[:, 1:], H.t[:, 1:])
 
 

@@ -95,8 +95,8 @@ def test_gated_refusals():
         (dict(X=None), I), (dict(Wg=None), I), (dict(Wu=None), I), (dict(H=None), I), (dict(act=4), I), (dict(act=-1), I), (dict(dt=5), I), (dict(N=0), I),
         (dict(M=0), I), (dict(S=0), I), (dict(H=p(1)), I), (dict(Z=p(4)), I), (dict(Z=p(1)), I), (dict(M=32769), U), (dict(S=65537), U),
         (dict(Wu=p(3) + 2), A), (dict(bg=p(7) + 4), A), (dict(Z=p(5) + 8), A)])
-    assert b.fw_workspace_bytes(b.FW_OP_GATED_FORWARD, 8, 6, b.conv_desc(40, 8)) > 0
-    statuses(L.fw_gated_forward, good, [(dict(N=40, ws=None), W), (dict(N=40, n=0), W)])
+    assert b.fw_workspace_bytes(b.FW_OP_GATED_FORWARD, 8, 6, b.conv_desc(100, 8)) > 0
+    statuses(L.fw_gated_forward, good, [(dict(N=100, ws=None), W), (dict(N=100, n=0), W)])
     good = dict(X=p(1), dt=1, N=4, M=8, S=6, Wg=p(2), Wu=p(3), Z=p(4), dH=p(5), mu=None, dX=p(6), dWg=p(7), dWu=p(8), dbg=p(9), dbu=p(10), ws=p(11),
                 n=1 << 20, stream=None)
     statuses(L.fw_gated_grad, good, [
