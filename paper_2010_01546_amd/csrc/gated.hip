@@ -10,7 +10,8 @@
 // rounded D, so that the identity is exact but for float32 sums.
 // float32: the same products with every operand as three bfloat16 planes (tile_product.h), split in one pass over X and the weights, D
 // when it is formed.  X is centred on mu as it is split.
-// float32 with few rows: float32 matrix instructions on the operands as they are (few_product_kernel), one row without them.
+// float32 with few rows: float32 matrix instructions on the operands as they are (few_product_kernel, few_rows_grad_kernel,
+// few_weights_grad_kernel), the projections of one row without them.
 #include "fw_internal.h"
 #include "tile_product.h"
 
@@ -48,9 +49,8 @@ template <class F> __device__ __forceinline__ void with_activation(int act, cons
 
 // ---- epilogues: four entries of a row.  FIX (operands in planes: an infinite number has none): entries that are not finite are computed
 // once more, in float32.
-__device__ __forceinline__ bool all_finite(const floatx4& v) {
-    return fabsf(v[0]) <= 3.402823466e38f && fabsf(v[1]) <= 3.402823466e38f && fabsf(v[2]) <= 3.402823466e38f && fabsf(v[3]) <= 3.402823466e38f;
-}
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+__device__ __forceinline__ bool all_finite(const floatx4& v) { return finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]); }
 template <class T, bool FIX> struct GateEpilogue {
     T* H;
     float* Z;
@@ -67,7 +67,10 @@ template <class T, bool FIX> struct GateEpilogue {
     __device__ __forceinline__ void apply(int n, int s, floatx4 gate, floatx4 up) const {
         if (n >= N || s >= S) return;
         if (FIX && !(all_finite(gate) && all_finite(up))) {
-            for (int i = 0; i < 4 && s + i < S; ++i) { gate[i] = dot(n, s + i, false); up[i] = dot(n, s + i, true); }
+            for (int i = 0; i < 4 && s + i < S; ++i) {
+                if (!finite(gate[i])) gate[i] = dot(n, s + i, false);
+                if (!finite(up[i])) up[i] = dot(n, s + i, true);
+            }
         }
         float b[4], c[4], h[4];
         tile_vector(bg, s, S, b);
@@ -109,7 +112,8 @@ template <class T, bool FIX> struct RowsEpilogue {           // dX
     __device__ __forceinline__ void apply(int n, int m, floatx4 acc) const {
         if (n >= N || m >= M) return;
         if (FIX && !all_finite(acc))
-            for (int i = 0; i < 4 && m + i < M; ++i) acc[i] = dot(n, m + i);
+            for (int i = 0; i < 4 && m + i < M; ++i)
+                if (!finite(acc[i])) acc[i] = dot(n, m + i);
         const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
         tile_store(out + (size_t)n * M + m, m, M, v);
     }
@@ -131,17 +135,17 @@ template <class T, bool FIX> struct WeightsEpilogue {        // rows below Sp ar
     __device__ __forceinline__ void apply(int r, int m, floatx4 acc) const {
         const int s = r >= Sp ? r - Sp : r;
         if (s >= S || m >= M) return;
-        const bool again = FIX && !all_finite(acc);
-        if (again)
-            for (int i = 0; i < 4 && m + i < M; ++i) acc[i] = dot(s, r >= Sp, m + i);
         float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-        if (mu && !again) {
+        if (mu) {
             const float d = sums[r];
             float c[4];
             tile_vector(mu, m, M, c);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] -= d * c[i];
         }
+        if (FIX && !all_finite(floatx4{v[0], v[1], v[2], v[3]}))
+            for (int i = 0; i < 4 && m + i < M; ++i)
+                if (!finite(v[i])) v[i] = dot(s, r >= Sp, m + i);
         tile_store((r >= Sp ? dWu : dWg) + (size_t)s * M + m, m, M, v);
     }
 };
@@ -324,6 +328,183 @@ __global__ __launch_bounds__(1024) void bias_grad_kernel(const float* __restrict
     else if (c % Sp < S) (c >= Sp ? dbu : dbg)[c % Sp] = (T)v;
 }
 
+// ---- float32 gradients of few rows, on the float32 matrix instructions and the weights as they are.
+// D[block of 16 s][gate, up][block of 16 n][lane][i] = dg or du of row n = lane % 16 and s = 4 (lane / 16) + i of the blocks, zeros past N and S:
+// the second operand of four v_mfma_f32_16x16x4_f32, 1 KB that a wavefront loads at once.  dbg, dbu: sums over the rows, or null.
+// A workgroup has a block of 16 s, a wavefront 16 rows of it.
+__global__ __launch_bounds__(256) void few_pack_kernel(const float* __restrict__ dH, const float* __restrict__ Z, int N, int S, float* __restrict__ D,
+                                                       float* __restrict__ dbg, float* __restrict__ dbu) {
+    __shared__ float red[4][2][16];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, a = threadIdx.x >> 6, NA = blockDim.x >> 6;
+    const int n = 16 * a + l16, s = 16 * blockIdx.x + 4 * q;
+    float d[2][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                    // loads of clamped places rather than branches: all of them go out together
+        const bool in = n < N && s + i < S;
+        const size_t e = (size_t)min(n, N - 1) * S + min(s + i, S - 1);
+        const float h = dH[e], z = Z[e], y = Z[(size_t)N * S + e];
+        d[0][i] = in ? h * z : 0.f;
+        d[1][i] = in ? h * y : 0.f;
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) *reinterpret_cast<float4*>(D + (((size_t)blockIdx.x * 2 + g) * NA + a) * 256 + 4 * lane) = make_float4(d[g][0], d[g][1], d[g][2], d[g][3]);
+    if (!dbg) return;
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int k = 1; k < 16; k *= 2) d[g][i] += __shfl_xor(d[g][i], k);
+            if (l16 == 0) red[a][g][4 * q + i] = d[g][i];
+        }
+    __syncthreads();
+    const int t = threadIdx.x, to = 16 * blockIdx.x + (t & 15);
+    if (t >= 32 || to >= S) return;
+    float v = red[0][t >> 4][t & 15];
+    for (int k = 1; k < NA; ++k) v += red[k][t >> 4][t & 15];
+    (t >> 4 ? dbu : dbg)[to] = v;
+}
+
+// dX (one row of 4172 features, 7040: 60 us, 3.9 TB/s of the weights): a workgroup has 64 columns and a run of blocks of s, its wavefronts take these in turn and add up their sums.  A lane holds four columns
+// next to each other of the rows 4 q + i of a block (whole cache lines); the last lanes' are moved back to end with the row, so that some
+// columns are computed twice, alike.  out: dX, or [run][N][M].
+template <int NA>
+__global__ __launch_bounds__(512) void few_rows_grad_kernel(const float* __restrict__ D, const float* __restrict__ Wg, const float* __restrict__ Wu,
+                                                            int N, int M, int S, int per_run, float* __restrict__ out) {
+    constexpr int NW = 8;
+    __shared__ floatx4 red[NW][4][64];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
+    const int m0 = blockIdx.x * 64, m = min(m0 + 4 * l16, M - 4);
+    const int blocks = (S + 15) / 16, end = min(((int)blockIdx.y + 1) * per_run, blocks);
+    floatx4 acc[NA][4];
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[a][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const auto load = [&](floatx4 (&w)[2][4], int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int s = 16 * b + 4 * q + i;
+                const float* p = (g ? Wu : Wg) + (size_t)s * M + m;
+                __builtin_memcpy(&w[g][i], b < end && s < S ? reinterpret_cast<const char*>(p) : reinterpret_cast<const char*>(&tile_zero), 16);
+            }
+    };
+    floatx4 w[2][4], next[2][4];
+    load(next, blockIdx.y * per_run + wave);
+    for (int b = blockIdx.y * per_run + wave; b < end; b += NW) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k >> 2][k & 3] = next[k >> 2][k & 3];
+        load(next, b + NW);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int a = 0; a < NA; ++a) {
+                const floatx4 d = *reinterpret_cast<const floatx4*>(D + (((size_t)b * 2 + g) * NA + a) * 256 + 4 * lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[a][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[g][i][j], d[i], acc[a][j], 0, 0, 0);
+            }
+    }
+    out += (size_t)blockIdx.y * N * M;
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+        if (a) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) red[wave][j][lane] = acc[a][j];
+        __syncthreads();
+        if (wave < 4 && 16 * a + l16 < N) {
+            floatx4 v = red[0][wave][lane];
+#pragma unroll
+            for (int k = 1; k < NW; ++k)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] += red[k][wave][lane][r];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int c = m0 + 4 * (4 * q + r);
+                if (c < M) out[(size_t)(16 * a + l16) * M + min(c, M - 4) + wave] = v[r];
+            }
+        }
+    }
+}
+
+// out[e] = the runs' sums, in order
+__global__ __launch_bounds__(256) void few_sum_kernel(const float* __restrict__ part, int runs, int n, float* __restrict__ out) {
+    const int e = blockIdx.x * 256 + threadIdx.x;
+    if (e >= n) return;
+    float v = part[e];
+    for (int r = 1; r < runs; ++r) v += part[(size_t)r * n + e];
+    out[e] = v;
+}
+
+// dWg and dWu: a wavefront has 64 x 64 entries of both, a workgroup two times two of these.  Bound by writing them (one row, 4172 features, 7040:
+// 85 us, 2.8 TB/s), from about 50 rows on by the matrix instructions.
+__global__ __launch_bounds__(256) void few_weights_grad_kernel(const float* __restrict__ D, int NA, const float* __restrict__ X, const float* __restrict__ mu, int N, int M,
+                                                               int S, float* __restrict__ dWg, float* __restrict__ dWu) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
+    const int m0 = blockIdx.x * 128 + 64 * (wave & 1), s0 = blockIdx.y * 128 + 64 * (wave >> 1), blocks = (S + 15) / 16;
+    if (m0 >= M || s0 >= S) return;
+    int m[4];
+    float c[4];
+    const float* d[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        m[j] = min(m0 + 16 * j + l16, M - 1);
+        c[j] = mu ? mu[m[j]] : 0.f;
+        d[j] = D + (size_t)min(s0 / 16 + j, blocks - 1) * 2 * NA * 256 + 64 * (l16 >> 2) + (l16 & 3);
+    }
+    floatx4 acc[2][4][4];
+#pragma unroll
+    for (int k = 0; k < 32; ++k) acc[k >> 4][(k >> 2) & 3][k & 3] = floatx4{0.f, 0.f, 0.f, 0.f};
+    struct Step { float x[4], y[2][4]; };
+    const auto load = [&](Step& t, int n) __attribute__((always_inline)) {
+        const int nx = min(n, N - 1), ny = min(n, 16 * NA - 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            t.x[j] = X[(size_t)nx * M + m[j]];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) t.y[g][j] = d[j][(g * NA + ny / 16) * 256 + 4 * (ny % 16)];
+        }
+    };
+    constexpr int AHEAD = 4;
+    Step step[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) load(step[k], 4 * k + q);
+    for (int n0 = 0; n0 < N; n0 += 4 * AHEAD) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int n = n0 + 4 * k + q;
+            float x[4], y[2][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {            // rows past the end: zeros of both
+                x[j] = n < N ? step[k].x[j] - c[j] : 0.f;
+                y[0][j] = n < N ? step[k].y[0][j] : 0.f;
+                y[1][j] = n < N ? step[k].y[1][j] : 0.f;
+            }
+            load(step[k], n + 4 * AHEAD);
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[g][i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[g][i], acc[g][i][j], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int s = s0 + 16 * i + l16;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float v[4] = {acc[g][i][j][0], acc[g][i][j][1], acc[g][i][j][2], acc[g][i][j][3]};
+                if (s < S) tile_store((g ? dWu : dWg) + (size_t)s * M + m0 + 16 * j + 4 * q, m0 + 16 * j + 4 * q, M, v);
+            }
+        }
+}
+
 // matrices of M bfloat16 columns to rows of Mp (a multiple of 8), zeros behind; the matrix goes by blockIdx.y
 struct Pad { const __bf16* in[3]; bf16x8* out[3]; int R[3]; };
 __global__ __launch_bounds__(256) void pad_rows_kernel(Pad s, int M, int Mp) {
@@ -344,9 +525,10 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(Pad s, int M, int Mp) {
     }
 }
 
-// Up to 64 rows float32 products are bound by the one read of the weights or nearly so; in planes these are written and read again (4172
-// features to 7040, 17 rows: 202 us against 68.6, 64 rows: 204 against 118, 86 rows: 215 against 200, 128 rows of 1153 to 1001: 27 against 37).
-constexpr int FEW_F32 = 64;
+// float32 projections on the operands as they are: up to 64 rows, which the one read of the weights bounds or nearly so; in planes these are
+// written and read again (4172 features to 7040, 17 rows: 202 us against 68.6, 64 rows: 204 against 117, 86 rows: 215 against 200).  More than
+// 32 rows of few columns are too few workgroups (64 x 4000 to 64: 22.6 us in planes against 43).
+inline bool few_forward(int N, int S) { return N <= 32 || (N <= 64 && S >= 256); }
 
 inline unsigned blocks_for(size_t n) { return (unsigned)((n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384); }
 inline int up8(int m) { return (m + 7) / 8 * 8; }
@@ -418,13 +600,25 @@ TileProduct weights_plan(fw_dtype dt, int N, int M, int S) {
     return g;
 }
 
+// float32 gradients on the operands as they are.  Both of 4172 features to 7040, one row: 387 us in planes against 151; 64 rows: 392 against 279,
+// of 576 to 2304: 59 against 55, of 300 to 1000: 44 against 50.  (86 rows as eight blocks of 16: no faster than in planes.)
+inline bool few_grad(fw_dtype dt, int N, int M, int S) {
+    return dt == FW_F32 && M >= 4 && (N <= 32 || (N <= 64 && (long long)M * S >= 1 << 20));
+}
+// blocks of 16 rows, and runs of blocks of s that give each of 512 workgroups two blocks a wavefront or more
+inline int few_blocks(int N) { return N <= 16 ? 1 : N <= 32 ? 2 : 4; }
+inline int few_runs(int M, int S) {
+    const int most = (S + 15) / 16 / 16, want = 512 / ((M + 63) / 64), runs = want < most ? want : most;
+    return runs > 1 ? runs : 1;
+}
+
 size_t plane3_bytes(int R, int M) { return 6 * (size_t)R * up64(M); }
 struct ForwardWs { void *X, *Wg, *Wu, *partial; size_t total; };
 ForwardWs forward_ws(fw_dtype dt, int N, int M, int S, void* ws) {
     Carve c = {reinterpret_cast<char*>(ws)};
     ForwardWs w = {};
     if (dt == FW_F32) {
-        if (N > FEW_F32) {
+        if (!few_forward(N, S)) {
             w.X = c.take(plane3_bytes(N, M));
             w.Wg = c.take(plane3_bytes(S, M));
             w.Wu = c.take(plane3_bytes(S, M));
@@ -434,7 +628,7 @@ ForwardWs forward_ws(fw_dtype dt, int N, int M, int S, void* ws) {
         w.Wg = c.take((size_t)S * up8(M) * 2);
         w.Wu = c.take((size_t)S * up8(M) * 2);
     }
-    if (N > (dt == FW_BF16 ? TILE_FEW : FEW_F32)) w.partial = c.take(tile_partial_bytes(forward_plan(dt, N, M, S)));
+    if (dt == FW_BF16 ? N > TILE_FEW : !few_forward(N, S)) w.partial = c.take(tile_partial_bytes(forward_plan(dt, N, M, S)));
     w.total = c.used;
     return w;
 }
@@ -443,6 +637,12 @@ GradWs grad_ws(fw_dtype dt, int N, int M, int S, void* ws) {
     Carve c = {reinterpret_cast<char*>(ws)};
     GradWs w = {};
     const size_t Sp = up64(S);
+    if (few_grad(dt, N, M, S)) {
+        w.D = c.take((size_t)((S + 15) / 16) * 2 * few_blocks(N) * 1024);
+        w.partial = c.take(few_runs(M, S) > 1 ? (size_t)few_runs(M, S) * N * M * 4 : 0);
+        w.total = c.used;
+        return w;
+    }
     w.D = c.take(dt == FW_F32 ? plane3_bytes(up64(N), 2 * (int)Sp) : (size_t)N * 2 * Sp * (two_planes(dt, N, S) ? 4 : 2));
     w.part = reinterpret_cast<float*>(c.take((size_t)row_blocks(N, S) * 4 * Sp * 4));
     w.sums = reinterpret_cast<float*>(c.take(2 * Sp * 4));
@@ -464,7 +664,7 @@ GradWs grad_ws(fw_dtype dt, int N, int M, int S, void* ws) {
 fw_status forward_f32(const float* X, int N, int M, int S, const float* Wg, const float* Wu, const float* bg, const float* bu, fw_act act,
                       float* H, float* Z, void* ws, hipStream_t st) {
     const ForwardWs w = forward_ws(FW_F32, N, M, S, ws);
-    if (N <= FEW_F32) {
+    if (few_forward(N, S)) {
         const GateEpilogue<float, false> epi = {H, Z, bg, bu, N, S, (int)act};
         const FewProduct few = {bytes(X), bytes(Wg), bytes(Wu), N, S, 4 * M};
         if (N > 32) return few_product<TILE_F32, true, 4>(few, epi, st);
@@ -528,6 +728,32 @@ fw_status gate_grad(const T* dH, const float* Z, int N, int S, const GradWs& w, 
 fw_status grad_f32(const float* X, int N, int M, int S, const float* Wg, const float* Wu, const float* Z, const float* dH, const float* mu,
                    float* dX, float* dWg, float* dWu, float* dbg, float* dbu, void* ws, hipStream_t st) {
     const GradWs w = grad_ws(FW_F32, N, M, S, ws);
+    if (few_grad(FW_F32, N, M, S)) {
+        const auto with_blocks = [&](auto NA) {
+            constexpr int na = decltype(NA)::value;
+            float* D = reinterpret_cast<float*>(w.D);
+            hipLaunchKernelGGL(few_pack_kernel, dim3((S + 15) / 16), dim3(64 * na), 0, st, dH, Z, N, S, D, dbg, dbu);
+            FW_LAUNCH_CHECK();
+            if (dX) {
+                const int want = few_runs(M, S), per = ((S + 15) / 16 + want - 1) / want, runs = ((S + 15) / 16 + per - 1) / per;
+                hipLaunchKernelGGL(few_rows_grad_kernel<na>, dim3((M + 63) / 64, runs), dim3(512), 0, st, D, Wg, Wu, N, M, S, per,
+                                   runs > 1 ? reinterpret_cast<float*>(w.partial) : dX);
+                FW_LAUNCH_CHECK();
+                if (runs > 1) {
+                    hipLaunchKernelGGL(few_sum_kernel, dim3((N * M + 255) / 256), dim3(256), 0, st, reinterpret_cast<const float*>(w.partial), runs, N * M, dX);
+                    FW_LAUNCH_CHECK();
+                }
+            }
+            if (dWg) {
+                hipLaunchKernelGGL(few_weights_grad_kernel, dim3((M + 127) / 128, (S + 127) / 128), dim3(256), 0, st, D, na, X, mu, N, M, S, dWg, dWu);
+                FW_LAUNCH_CHECK();
+            }
+            return FW_OK;
+        };
+        if (N <= 16) return with_blocks(std::integral_constant<int, 1>());
+        if (N <= 32) return with_blocks(std::integral_constant<int, 2>());
+        return with_blocks(std::integral_constant<int, 4>());
+    }
     const int Sp = up64(S), Np = up64(N);
     fw_status rc = gate_grad<float>(dH, Z, N, S, w, false, dbg, dbu, st);
     if (rc != FW_OK) return rc;

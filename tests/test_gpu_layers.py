@@ -176,7 +176,7 @@ def test_int8_rows(N, M, dtype):
 
 GATED_SIZES = [(1, 1, 1), (1, 8, 5), (1, 64, 128), (2, 33, 65), (3, 130, 64), (7, 256, 200), (16, 576, 96), (17, 72, 257), (31, 1000, 33),
                (32, 512, 512), (33, 40, 130), (64, 64, 64), (65, 96, 129), (127, 129, 513), (128, 576, 256), (130, 200, 1000), (200, 1153, 67),
-               (257, 320, 384), (300, 72, 700), (513, 257, 300), (1100, 64, 72), (1, 2304, 300), (4, 4608, 40), (520, 513, 1030)]
+               (257, 320, 384), (300, 72, 700), (513, 257, 300), (1100, 64, 72), (1, 2304, 300), (4, 4608, 40), (520, 513, 1030), (1, 3, 70), (18, 4, 33), (40, 1030, 1100), (64, 4099, 300), (64, 2001, 130), (9, 70, 4100)]
 ACT = {k: i for i, k in enumerate(lo.ACTS)}
 
 
