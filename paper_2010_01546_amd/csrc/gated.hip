@@ -47,10 +47,33 @@ template <class F> __device__ __forceinline__ void with_activation(int act, cons
     else f(std::integral_constant<int, FW_ACT_RELU>());
 }
 
-// ---- epilogues: four entries of a row.  FIX (operands in planes: an infinite number has none): entries that are not finite are computed
-// once more, in float32.
+// ---- epilogues: four entries of a row, 16 x 16 of a wavefront.  FIX (operands in planes: an infinite number has none): where an entry of the 16 x
+// 16 is not finite they are computed once more on the float32 matrix instructions, and those entries replaced.  (Entry by entry would take
+// minutes for a large matrix full of NaN.)
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
-__device__ __forceinline__ bool all_finite(const floatx4& v) { return finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]); }
+__device__ __forceinline__ bool not_finite(const floatx4& v) {
+    return __builtin_amdgcn_ballot_w64(!(finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]))) != 0;
+}
+// adds 16 x 16 results: row(k), column(k): the entries at k of the lane's row, of its 16 lanes' column
+template <class Row, class Column> __device__ __forceinline__ void block_in_f32(floatx4& acc, int K, const Row& row, const Column& column) {
+    const int q = (threadIdx.x & 63) >> 4;
+#pragma unroll 4
+    for (int k0 = 0; k0 < K; k0 += 4) {
+        const int k = min(k0 + q, K - 1);
+        const bool in = k0 + q < K;
+        const float x = column(k), y = row(k);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? x : 0.f, in ? y : 0.f, acc, 0, 0, 0);
+    }
+}
+// the column that a lane brings, where its results begin at column c
+__device__ __forceinline__ int column_of(int c, int columns) {
+    const int lane = threadIdx.x & 63;
+    return min(c - 4 * (lane >> 4) + (lane & 15), columns - 1);
+}
+__device__ __forceinline__ void replace(floatx4& v, const floatx4& by) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = finite(v[i]) ? v[i] : by[i];
+}
 template <class T, bool FIX> struct GateEpilogue {
     T* H;
     float* Z;
@@ -58,20 +81,16 @@ template <class T, bool FIX> struct GateEpilogue {
     int N, S, act;
     const float *X, *Wg, *Wu;             // FIX: the operands as they were
     int M;
-    __device__ __noinline__ float dot(int n, int s, bool up) const {
-        const float *x = X + (size_t)n * M, *w = (up ? Wu : Wg) + (size_t)s * M;
-        float v = 0.f;
-        for (int m = 0; m < M; ++m) v = fmaf(x[m], w[m], v);
+    __device__ __noinline__ floatx4 again(int n, int s, const float* W) const {
+        const float *x = X + (size_t)min(n, N - 1) * M, *w = W + (size_t)column_of(s, S) * M;
+        floatx4 v = {0.f, 0.f, 0.f, 0.f};
+        block_in_f32(v, M, [&](int m) { return x[m]; }, [&](int m) { return w[m]; });
         return v;
     }
     __device__ __forceinline__ void apply(int n, int s, floatx4 gate, floatx4 up) const {
+        if (FIX && not_finite(gate)) replace(gate, again(n, s, Wg));
+        if (FIX && not_finite(up)) replace(up, again(n, s, Wu));
         if (n >= N || s >= S) return;
-        if (FIX && !(all_finite(gate) && all_finite(up))) {
-            for (int i = 0; i < 4 && s + i < S; ++i) {
-                if (!finite(gate[i])) gate[i] = dot(n, s + i, false);
-                if (!finite(up[i])) up[i] = dot(n, s + i, true);
-            }
-        }
         float b[4], c[4], h[4];
         tile_vector(bg, s, S, b);
         tile_vector(bu, s, S, c);
@@ -100,20 +119,18 @@ template <class T, bool FIX> struct RowsEpilogue {           // dX
     T* out;
     int N, M;
     GradInputs<T> in;
-    __device__ __noinline__ float dot(int n, int m) const {
-        float v = 0.f;
-        for (int s = 0; s < in.S; ++s) {
-            const size_t e = (size_t)n * in.S + s, w = (size_t)s * M + m;
-            v = fmaf((float)in.dH[e] * in.Z[e], (float)in.Wg[w], v);
-            v = fmaf((float)in.dH[e] * in.Z[(size_t)N * in.S + e], (float)in.Wu[w], v);
-        }
+    __device__ __noinline__ floatx4 again(int n, int m) const {
+        const size_t at = (size_t)min(n, N - 1) * in.S;
+        const int c = column_of(m, M);
+        floatx4 v = {0.f, 0.f, 0.f, 0.f};
+        block_in_f32(v, in.S, [&](int s) { return (float)in.dH[at + s] * in.Z[at + s]; }, [&](int s) { return (float)in.Wg[(size_t)s * M + c]; });
+        block_in_f32(v, in.S, [&](int s) { return (float)in.dH[at + s] * in.Z[(size_t)N * in.S + at + s]; },
+                     [&](int s) { return (float)in.Wu[(size_t)s * M + c]; });
         return v;
     }
     __device__ __forceinline__ void apply(int n, int m, floatx4 acc) const {
+        if (FIX && not_finite(acc)) replace(acc, again(n, m));
         if (n >= N || m >= M) return;
-        if (FIX && !all_finite(acc))
-            for (int i = 0; i < 4 && m + i < M; ++i)
-                if (!finite(acc[i])) acc[i] = dot(n, m + i);
         const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
         tile_store(out + (size_t)n * M + m, m, M, v);
     }
@@ -123,30 +140,28 @@ template <class T, bool FIX> struct WeightsEpilogue {        // rows below Sp ar
     const float *sums, *mu;               // mu: taken out here (bfloat16), or null
     int S, Sp, M;
     GradInputs<T> in;
-    __device__ __noinline__ float dot(int s, bool up, int m) const {
-        const float c = in.mu ? in.mu[m] : 0.f;
-        float v = 0.f;
-        for (int n = 0; n < in.N; ++n) {
-            const size_t e = (size_t)n * S + s;
-            v = fmaf((float)in.dH[e] * in.Z[(up ? (size_t)in.N * S : 0) + e], (float)in.X[(size_t)n * M + m] - c, v);
-        }
+    __device__ __noinline__ floatx4 again(int s, bool up, int m) const {
+        const size_t at = (up ? (size_t)in.N * S : 0) + s;
+        const int c = column_of(m, M);
+        const float mean = in.mu ? in.mu[c] : 0.f;
+        floatx4 v = {0.f, 0.f, 0.f, 0.f};
+        block_in_f32(v, in.N, [&](int n) { return (float)in.dH[(size_t)n * S + s] * in.Z[(size_t)n * S + at]; },
+                     [&](int n) { return (float)in.X[(size_t)n * M + c] - mean; });
         return v;
     }
-    __device__ __forceinline__ void apply(int r, int m, floatx4 acc) const {
+    __device__ __forceinline__ void apply(int r, int m, floatx4 v) const {
         const int s = r >= Sp ? r - Sp : r;
-        if (s >= S || m >= M) return;
-        float v[4] = {acc[0], acc[1], acc[2], acc[3]};
         if (mu) {
-            const float d = sums[r];
+            const float d = sums[min(r, 2 * Sp - 1)];
             float c[4];
             tile_vector(mu, m, M, c);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] -= d * c[i];
         }
-        if (FIX && !all_finite(floatx4{v[0], v[1], v[2], v[3]}))
-            for (int i = 0; i < 4 && m + i < M; ++i)
-                if (!finite(v[i])) v[i] = dot(s, r >= Sp, m + i);
-        tile_store((r >= Sp ? dWu : dWg) + (size_t)s * M + m, m, M, v);
+        if (FIX && not_finite(v)) replace(v, again(min(s, S - 1), r >= Sp, m));
+        if (s >= S || m >= M) return;
+        const float out[4] = {v[0], v[1], v[2], v[3]};
+        tile_store((r >= Sp ? dWu : dWg) + (size_t)s * M + m, m, M, out);
     }
 };
 

@@ -451,6 +451,27 @@ def test_gated_with_infinite_and_nan_entries(N, M, S, dtype):
         assert fine.any() and relF(got[fine], w[fine]) < (2 * HALF["bf16"] if dtype == "bf16" else 1e-5), what
 
 
+@pytest.mark.parametrize("N,M,S", [(150, 257, 300), (1000, 4608, 4000)])
+def test_gated_of_nan(N, M, S):
+    """float32, not a finite result: as the formula has it, and in a time like that of any other input."""
+    t = lambda *shape: torch.full(shape, float("nan"), device=DEV)  # noqa: E731
+    H, Z, dX, dWg, dWu = (Out(*shape, dtype=torch.float32) for shape in ((N, S), (2, N, S), (N, M), (S, M), (S, M)))
+    X, W, dH = t(N, M), torch.ones(S, M, device=DEV), torch.ones(N, S, device=DEV)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_FORWARD, M, S, b.conv_desc(N, M)))
+    b.fw_gated_forward(X, b.FW_F32, N, M, S, W, W, None, None, b.FW_ACT_SILU, H.t, Z.t, ws)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_GRAD, M, S, b.conv_desc(N, M)))
+    b.fw_gated_grad(X, b.FW_F32, N, M, S, W, W, Z.t, dH, None, dX.t, dWg.t, dWu.t, None, None, ws)
+    torch.cuda.synchronize()
+    for x in (H, Z, dX, dWg, dWu):
+        assert bool(torch.isnan(x.t).all())
+    begin, end = torch.cuda.Event(True), torch.cuda.Event(True)
+    begin.record()
+    b.fw_gated_grad(X, b.FW_F32, N, M, S, W, W, Z.t, dH, None, dX.t, dWg.t, dWu.t, None, None, ws)
+    end.record()
+    torch.cuda.synchronize()
+    assert begin.elapsed_time(end) < 100                           # ms; entry by entry it would be seconds
+
+
 def test_offsets_beyond_32_bits():
     """Rows at the end of tensors of more than 2^31 entries."""
     t, dt = torch.bfloat16, b.FW_BF16
