@@ -22,7 +22,7 @@
 //   panels; of their nine products the six above 2^-24 go into the same float32 sums: l h, m h, h h, h m, m m, h l.  (Every pair of planes
 //   as a product of its own, each with its loads: 1024 x 576 x 2304, 61 us forward; loads bound it.)  The planes are padded with zeros to
 //   whole stages.  Entries below 2^-110 lose their last bits (bfloat16 ends at 2^-133); where a result is not finite (an infinite entry
-//   has no such sum) the epilogue computes it once more in float32.
+//   has no such sum) the epilogue computes its 16 x 16 once more in float32.
 // Two operands A may meet the same B one after the other (once): sums of a product whose A is the sum of two bfloat16 numbers.
 // Where the contraction ends inside a stage, the loads past the end fetch a zero (in both operands: 0 x NaN is NaN).  Rows or columns past
 // the edge are clamped; they feed results that the epilogue does not store.
