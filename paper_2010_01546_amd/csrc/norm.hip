@@ -326,7 +326,7 @@ inline int grad_blocks(int N, int M) {
 inline int up4(int m) { return (m + 3) / 4 * 4; }
 
 // calls f(threads of a row, accesses of each, how rows end): as few accesses of 8 entries as hold the row, which ends in the last of them.  (4608 features: 256 threads with
-// three accesses, 58 us for 8192 rows; 320 with two, 77 us.)
+// three accesses, 58 us for 8192 rows; 320 with two, 77 us.  2048 gradient rows of 12288: 512 with three, 46.6 us; 1024 with two, 55.)
 template <class F> void with_shape(int M, const F& f) {
     using std::integral_constant;
     auto with_end = [&](auto G, auto NV) {
@@ -341,7 +341,8 @@ template <class F> void with_shape(int M, const F& f) {
     else if (M <= 4096) with_end(integral_constant<int, 256>(), integral_constant<int, 2>());
     else if (M <= 6144) with_end(integral_constant<int, 256>(), integral_constant<int, 3>());
     else if (M <= 8192) with_end(integral_constant<int, 512>(), integral_constant<int, 2>());
-    else if (M <= 16384) with_end(integral_constant<int, 1024>(), integral_constant<int, 2>());
+    else if (M <= 12288) with_end(integral_constant<int, 512>(), integral_constant<int, 3>());
+    else if (M <= 16384) with_end(integral_constant<int, 512>(), integral_constant<int, 4>());
     else if (M <= 24576) with_end(integral_constant<int, 1024>(), integral_constant<int, 3>());
     else with_end(integral_constant<int, 1024>(), integral_constant<int, 4>());
 }

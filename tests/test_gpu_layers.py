@@ -51,7 +51,7 @@ def within(got, want, tol, what=""):
 # ---------------------------------------------------------------------------------------------------------------- norm
 
 NORM_SIZES = [(1, 1), (1, 7), (2, 8), (3, 64), (5, 129), (4, 512), (7, 513), (3, 1025), (6, 2048), (2, 2049), (1, 4608), (3, 8192), (2, 8197),
-              (2, 16384), (1, 16391), (2, 32768), (65, 48), (1030, 72), (4101, 33), (9, 9), (17, 507), (11, 2043), (9, 6139), (3, 16381), (3, 32763), (1035, 2307), (2, 16393), (2, 24577), (3, 24576)]
+              (2, 16384), (1, 16391), (2, 32768), (65, 48), (1030, 72), (4101, 33), (9, 9), (17, 507), (11, 2043), (9, 6139), (3, 16381), (3, 32763), (1035, 2307), (2, 16393), (2, 24577), (3, 24576), (2, 12285), (3, 12289)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
