@@ -359,7 +359,7 @@ fw_status fw_cond_probe(const float* Phi_y, int M, const float* b0, int k, float
  * (5) Layers of a language model around the whitening: what makes a layer's input rows X [N, M] (one row per token, the rows that
  * fw_cov_accumulate takes as FW_LAYOUT_ROWS), its products, its weight gradients G [S, M], and its answers in 8 bits.  N, M and S
  * need not be multiples of anything; the products copy their operands once to aligned rows where M is not a multiple of 8 (bfloat16)
- * or 16 (8 bits) and there are more than 16 rows.  Limits of all of them: N <= 2097152, M <= 32768,
+ * or 16 (8 bits) and the rows are many.  Limits of all of them: N <= 2097152, M <= 32768,
  * S <= 65536.  The workspaces are asked for with
  * d = {N, M, 1, 1, 1, 1, 1, 0, 0}, the geometry of N rows.
  *

@@ -543,7 +543,9 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(Pad s, int M, int Mp) {
 // float32 projections on the operands as they are: up to 64 rows, which the one read of the weights bounds or nearly so; in planes these are
 // written and read again (4172 features to 7040, 17 rows: 202 us against 68.6, 64 rows: 204 against 117, 86 rows: 215 against 200).  More than
 // 32 rows of few columns are too few workgroups (64 x 4000 to 64: 22.6 us in planes against 43).
-inline bool few_forward(int N, int S) { return N <= 32 || (N <= 64 && S >= 256); }
+inline bool few_forward(fw_dtype dt, int N, int M, int S) {
+    return dt == FW_F32 ? N <= 32 || (N <= 64 && S >= 256) : few_rows(N, S, M % 8 == 0, true);
+}
 
 inline unsigned blocks_for(size_t n) { return (unsigned)((n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384); }
 inline int up8(int m) { return (m + 7) / 8 * 8; }
@@ -632,18 +634,19 @@ struct ForwardWs { void *X, *Wg, *Wu, *partial; size_t total; };
 ForwardWs forward_ws(fw_dtype dt, int N, int M, int S, void* ws) {
     Carve c = {reinterpret_cast<char*>(ws)};
     ForwardWs w = {};
+    const bool few = few_forward(dt, N, M, S);
     if (dt == FW_F32) {
-        if (!few_forward(N, S)) {
+        if (!few) {
             w.X = c.take(plane3_bytes(N, M));
             w.Wg = c.take(plane3_bytes(S, M));
             w.Wu = c.take(plane3_bytes(S, M));
         }
-    } else if (M % 8 && N > TILE_FEW) {
+    } else if (M % 8 && !few) {
         w.X = c.take((size_t)N * up8(M) * 2);
         w.Wg = c.take((size_t)S * up8(M) * 2);
         w.Wu = c.take((size_t)S * up8(M) * 2);
     }
-    if (dt == FW_BF16 ? N > TILE_FEW : !few_forward(N, S)) w.partial = c.take(tile_partial_bytes(forward_plan(dt, N, M, S)));
+    if (!few) w.partial = c.take(tile_partial_bytes(forward_plan(dt, N, M, S)));
     w.total = c.used;
     return w;
 }
@@ -679,12 +682,10 @@ GradWs grad_ws(fw_dtype dt, int N, int M, int S, void* ws) {
 fw_status forward_f32(const float* X, int N, int M, int S, const float* Wg, const float* Wu, const float* bg, const float* bu, fw_act act,
                       float* H, float* Z, void* ws, hipStream_t st) {
     const ForwardWs w = forward_ws(FW_F32, N, M, S, ws);
-    if (few_forward(N, S)) {
+    if (few_forward(FW_F32, N, M, S)) {
         const GateEpilogue<float, false> epi = {H, Z, bg, bu, N, S, (int)act};
         const FewProduct few = {bytes(X), bytes(Wg), bytes(Wu), N, S, 4 * M};
-        if (N > 32) return few_product<TILE_F32, true, 4>(few, epi, st);
-        if (N > 16) return few_product<TILE_F32, true, 2>(few, epi, st);
-        if (N > 1) return few_product<TILE_F32, true, 1>(few, epi, st);
+        if (N > 1) return few_product<TILE_F32, true>(few, epi, st);
         hipLaunchKernelGGL(one_row_kernel, dim3((S + 3) / 4), dim3(256), 0, st, X, M, S, Wg, Wu, epi);
         FW_LAUNCH_CHECK();
         return FW_OK;
@@ -705,7 +706,7 @@ fw_status forward_bf16(const void* X, int N, int M, int S, const void* Wg, const
                        void* H, float* Z, void* ws, hipStream_t st) {
     const ForwardWs w = forward_ws(FW_BF16, N, M, S, ws);
     const GateEpilogue<__bf16, false> epi = {reinterpret_cast<__bf16*>(H), Z, bg, bu, N, S, (int)act};
-    if (N <= TILE_FEW) return few_product<TILE_BF16, true>({bytes(X), bytes(Wg), bytes(Wu), N, S, 2 * M}, epi, st);
+    if (few_forward(FW_BF16, N, M, S)) return few_product<TILE_BF16, true>({bytes(X), bytes(Wg), bytes(Wu), N, S, 2 * M}, epi, st);
     if (M % 8) {             // 16-byte loads need aligned rows
         PadList pads;
         pads.add(X, N, w.X);

@@ -62,14 +62,14 @@ size_t padded_bytes(int R, int M) { return M % 16 ? align_up((size_t)R * up16(M)
 }  // namespace
 
 size_t int8_product_workspace_bytes(int N, int M, int S) {
-    if (N <= TILE_FEW) return 0;
+    if (few_rows(N, S, M % 16 == 0, false)) return 0;
     return padded_bytes(N, M) + padded_bytes(S, M) + tile_partial_bytes(plan(N, M, S));
 }
 
 fw_status int8_product(const signed char* Xq, const float* sx, int N, int M, int S, const signed char* Wq, const float* sw, const float* b,
                        void* Y, fw_dtype dt, void* ws, hipStream_t st) {
     char* w = reinterpret_cast<char*>(ws);
-    if (N <= TILE_FEW) {
+    if (few_rows(N, S, M % 16 == 0, false)) {
         const FewProduct few = {reinterpret_cast<const char*>(Xq), reinterpret_cast<const char*>(Wq), nullptr, N, S, M};
         if (dt == FW_BF16) return few_product<TILE_I8, false>(few, ScaleEpilogue<__bf16>{reinterpret_cast<__bf16*>(Y), sx, sw, b, N, S}, st);
         return few_product<TILE_I8, false>(few, ScaleEpilogue<float>{reinterpret_cast<float*>(Y), sx, sw, b, N, S}, st);

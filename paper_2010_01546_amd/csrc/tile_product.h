@@ -493,8 +493,7 @@ fw_status tile_product(const TileProduct& g, const Epi& epi, hipStream_t st) {
 // row, so that whole cache lines are asked for) and add up their sums at the end: one launch, no workspace, no padded copies.
 // Two projections of one row of 4608 bfloat16, 12288 columns: 42.7 us, 5.3 TB/s; 16 rows of 12288 bytes, 4608 columns: 11.6 us, 4.9 TB/s.
 // (Tiles of 64 rows whose contraction is cut into runs: 43.7 and 18.0 us; 1 x 1153, 1001 columns, whose rows these need padded: 13.3
-// against 5.9.  32 rows by two tiles of 16: from 4608 x 2304 on slower than tiles of 64.)
-constexpr int TILE_FEW = 16;
+// against 5.9.)
 struct FewProduct {
     const char *a, *b0, *b1;
     int N, C, bytes, cols;        // rows, columns (PAIR: of each matrix), bytes of a row, columns of a workgroup
@@ -611,14 +610,28 @@ __global__ __launch_bounds__(512, NA > 1 ? 2 : 4) void few_product_kernel(FewPro
         }
     }
 }
-template <TileKind KIND, bool PAIR, int NA = 1, class Epi>
-fw_status few_product(FewProduct g, const Epi& epi, hipStream_t st) {
-    constexpr int MOST = PAIR ? 16 : 32;             // columns a workgroup can take
-    const int each = (g.C + 255) / 256, parts = (each + MOST - 1) / MOST;
+constexpr int few_most(bool pair) { return pair ? 16 : 32; }         // columns a workgroup can take
+// bfloat16 and 8 bits: few_product up to 16 rows; up to 64 where there are columns for every compute unit and, if the rows are aligned, not so
+// many that a unit takes them in several goes, each with its loads of A.  Tiles against this: projections of 32 rows, 1153 to 4001: 20.6 us and
+// 8.9, 2304 to 6145: 16.6 and 13.3, 4608 to 12288: 45.0 and 47.8, 64 to 200: 4.3 and 5.0; of 64 rows, 576 to 2304: 8.5 and 7.3, 2304 to 6145: 17.0
+// and 21.3, 2305 to 6145: 41 and 29; 8 bits, 64 rows, 4608 to 4608: 13.7 and 10.8, to 12288: 17.3 and 20.5.
+inline bool few_rows(int N, int C, bool aligned, bool pair) {
+    return N <= 16 || (N <= 64 && C >= 256 && (!aligned || C <= 256 * few_most(pair) * (N <= 32 ? 2 : 1)));
+}
+template <TileKind KIND, bool PAIR, int NA, class Epi>
+fw_status few_launch(FewProduct g, const Epi& epi, hipStream_t st) {
+    const int each = (g.C + 255) / 256, parts = (each + few_most(PAIR) - 1) / few_most(PAIR);
     g.cols = ((each + parts - 1) / parts + 3) / 4 * 4;
     hipLaunchKernelGGL((few_product_kernel<KIND, NA, PAIR, Epi>), dim3((g.C + g.cols - 1) / g.cols), dim3(512), 0, st, g, epi);
     FW_LAUNCH_CHECK();
     return FW_OK;
+}
+
+template <TileKind KIND, bool PAIR, class Epi>
+fw_status few_product(const FewProduct& g, const Epi& epi, hipStream_t st) {
+    if (g.N <= 16) return few_launch<KIND, PAIR, 1>(g, epi, st);
+    if (g.N <= 32) return few_launch<KIND, PAIR, 2>(g, epi, st);
+    return few_launch<KIND, PAIR, 4>(g, epi, st);
 }
 
 }  // namespace fw

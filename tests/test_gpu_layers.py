@@ -299,7 +299,7 @@ def test_gated_gradient(N, M, S, dtype):
 
 # few rows, where each workgroup has its columns' whole sums, and a few more: row ends of every kind, few and many columns
 FEW_SIZES = [(1, 7, 3), (2, 8, 259), (4, 33, 1), (15, 129, 300), (16, 577, 1030), (17, 1100, 33), (31, 136, 4100), (32, 2305, 6145), (3, 64, 8200),
-             (1, 12289, 20)]
+             (1, 12289, 20), (50, 129, 300), (64, 1000, 270), (40, 2305, 4200)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
