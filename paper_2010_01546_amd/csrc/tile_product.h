@@ -271,7 +271,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
         // half that follows the loads of B's stage c + D go out, in the half after that those of A's stage c + D + 1.  The loads of a wavefront
         // complete in order; with those behind B's stage c + 1 outstanding all of that stage has landed for it, the barrier extends that to
         // all.  Past the end the loads fetch zeros, which keeps their number the same.  (Small tiles gain from a deep ring: 501 x 2304 x
-        // 6145, two projections, 39.7 us with two stages, 36.6 with four.)
+        // 6145, two projections, 39.7 us with two stages of B, 36.6 with three.)
         auto load_panel = [&](auto ISA, int to_buf, int c) __attribute__((always_inline)) {
             const Stage s = stage_at(c);
 #pragma unroll
