@@ -428,6 +428,7 @@ fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, cons
  *   dWg, dWu    out  [S, M] element type `dt`, or both NULL
  *   dbg, dbu    out  [S] element type `dt`, or both NULL
  *   ws          scratch, fw_workspace_bytes(FW_OP_GATED_GRAD, M, S, d, dt) bytes
+ * The outputs overlap neither each other nor the inputs.
  * FW_BF16: dg and du are rounded to bfloat16 for the products (and for mu's part in them) where N S > 524288, below they are held as two
  * bfloat16 numbers each (the rounding would not average out); the sums are float32 and each result is rounded once; dbg and dbu are
  * sums of the values before that rounding.

@@ -348,7 +348,8 @@ fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const v
                         const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws, size_t ws_bytes, void* stream) {
     if (!X || !Wg || !Wu || !Z || !dH || !dWg != !dWu || !dbg != !dbu || (!dX && !dWg && !dbg)) return FW_ERR_INVALID_ARG;
     if (dX && (dX == X || dX == dH || dX == (const void*)Z || dX == Wg || dX == Wu || dX == dWg || dX == dWu)) return FW_ERR_INVALID_ARG;
-    if (dWg && (dWg == dWu || dWg == Wg || dWg == Wu || dWu == Wg || dWu == Wu || dWg == X || dWu == X)) return FW_ERR_INVALID_ARG;
+    if (dWg && (dWg == dWu || dWg == Wg || dWg == Wu || dWu == Wg || dWu == Wu || dWg == X || dWu == X || dWg == dH || dWu == dH || dWg == (const void*)Z || dWu == (const void*)Z))
+        return FW_ERR_INVALID_ARG;
     if (dbg && dbg == dbu) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, S);
     if (rc != FW_OK) return rc;

@@ -4,10 +4,12 @@
 //
 // bfloat16: both projections in one launch, the panel of weights holding the same columns of Wg and Wu, so that a lane has g and u of
 // an element in its registers when the sums are done (tile_product.h).  The backward pass forms D = [dg | du] once, rounded to
-// bfloat16 (small N S: to two bfloat16 numbers, see two_planes), [N][2 Sp] with Sp = S rounded up to 64 and zeros between, and takes two products of it: dX = D [Wg; Wu], whose contraction runs
-// over the rows of both weight matrices, and [dWg; dWu] = D^T X.  Operands that are contraction-major in memory are turned on the
-// way out of LDS, not in memory.  mu is taken out of the sums: D^T (X - 1 mu^T) = D^T X - (D^T 1) mu^T, with D^T 1 summed from the
-// rounded D, so that the identity is exact but for float32 sums.
+// bfloat16 (small N S: as two bfloat16 numbers, two_planes), [N][2 Sp] with Sp = S rounded up to 64 and zeros between, and takes two
+// products of it: dX = D [Wg; Wu], whose contraction runs over the rows of both weight matrices, and [dWg; dWu] = D^T X.  Operands that
+// are contraction-major in memory are turned on the way out of LDS, not in memory.  mu is taken out of the sums: D^T (X - 1 mu^T) =
+// D^T X - (D^T 1) mu^T, with D^T 1 summed from D as it is held, so that the identity is exact but for float32 sums.
+// 8192 x 4608 to 12288: projections 1470 us (1.26 PFLOP/s; 140 more with Z), D 275 (the rate of HBM), dX 1284 (1.45), dWg and dWu 1326 (1.40):
+// the power limit.
 // float32: the same products with every operand as three bfloat16 planes (tile_product.h), split in one pass over X and the weights, D
 // when it is formed.  X is centred on mu as it is split.
 // float32 with few rows: float32 matrix instructions on the operands as they are (few_product_kernel, few_rows_grad_kernel,
@@ -362,7 +364,8 @@ __global__ __launch_bounds__(256) void few_pack_kernel(const float* __restrict__
         d[1][i] = in ? h * y : 0.f;
     }
 #pragma unroll
-    for (int g = 0; g < 2; ++g) *reinterpret_cast<float4*>(D + (((size_t)blockIdx.x * 2 + g) * NA + a) * 256 + 4 * lane) = make_float4(d[g][0], d[g][1], d[g][2], d[g][3]);
+    for (int g = 0; g < 2; ++g)
+        *reinterpret_cast<float4*>(D + (((size_t)blockIdx.x * 2 + g) * NA + a) * 256 + 4 * lane) = make_float4(d[g][0], d[g][1], d[g][2], d[g][3]);
     if (!dbg) return;
 #pragma unroll
     for (int g = 0; g < 2; ++g)
@@ -380,9 +383,9 @@ __global__ __launch_bounds__(256) void few_pack_kernel(const float* __restrict__
     (t >> 4 ? dbu : dbg)[to] = v;
 }
 
-// dX (one row of 4172 features, 7040: 60 us, 3.9 TB/s of the weights): a workgroup has 64 columns and a run of blocks of s, its wavefronts take these in turn and add up their sums.  A lane holds four columns
-// next to each other of the rows 4 q + i of a block (whole cache lines); the last lanes' are moved back to end with the row, so that some
-// columns are computed twice, alike.  out: dX, or [run][N][M].
+// dX (one row of 4172 features, 7040: 60 us, 3.9 TB/s of the weights): a workgroup has 64 columns and a run of blocks of s, its wavefronts
+// take these in turn and add up their sums.  A lane holds four columns next to each other of the rows 4 q + i of a block (whole cache
+// lines); the last lanes' are moved back to end with the row, so that some columns are computed twice, alike.  out: dX, or [run][N][M].
 template <int NA>
 __global__ __launch_bounds__(512) void few_rows_grad_kernel(const float* __restrict__ D, const float* __restrict__ Wg, const float* __restrict__ Wu,
                                                             int N, int M, int S, int per_run, float* __restrict__ out) {
@@ -456,8 +459,9 @@ __global__ __launch_bounds__(256) void few_sum_kernel(const float* __restrict__ 
 
 // dWg and dWu: a wavefront has 64 x 64 entries of both, a workgroup two times two of these.  Bound by writing them (one row, 4172 features, 7040:
 // 85 us, 2.8 TB/s), from about 50 rows on by the matrix instructions.
-__global__ __launch_bounds__(256) void few_weights_grad_kernel(const float* __restrict__ D, int NA, const float* __restrict__ X, const float* __restrict__ mu, int N, int M,
-                                                               int S, float* __restrict__ dWg, float* __restrict__ dWu) {
+__global__ __launch_bounds__(256) void few_weights_grad_kernel(const float* __restrict__ D, int NA, const float* __restrict__ X,
+                                                               const float* __restrict__ mu, int N, int M, int S, float* __restrict__ dWg,
+                                                               float* __restrict__ dWu) {
     const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
     const int m0 = blockIdx.x * 128 + 64 * (wave & 1), s0 = blockIdx.y * 128 + 64 * (wave >> 1), blocks = (S + 15) / 16;
     if (m0 >= M || s0 >= S) return;

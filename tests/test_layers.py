@@ -102,7 +102,8 @@ def test_gated_refusals():
     statuses(L.fw_gated_grad, good, [
         (dict(X=None), I), (dict(Wg=None), I), (dict(Wu=None), I), (dict(Z=None), I), (dict(dH=None), I), (dict(dWg=None), I), (dict(dWu=None), I),
         (dict(dbg=None), I), (dict(dbu=None), I), (dict(dX=None, dWg=None, dWu=None, dbg=None, dbu=None), I), (dict(dX=p(1)), I), (dict(dX=p(5)), I),
-        (dict(dX=p(4)), I), (dict(dWg=p(8)), I), (dict(dWg=p(2)), I), (dict(dWu=p(2)), I), (dict(dWu=p(1)), I), (dict(dX=p(7)), I), (dict(dX=p(2)), I), (dict(dbu=p(9)), I), (dict(dt=2), I), (dict(N=0), I),
+        (dict(dX=p(4)), I), (dict(dWg=p(8)), I), (dict(dWg=p(2)), I), (dict(dWu=p(2)), I), (dict(dWu=p(1)), I), (dict(dX=p(7)), I), (dict(dX=p(2)), I),
+        (dict(dWg=p(5)), I), (dict(dWu=p(5)), I), (dict(dWg=p(4)), I), (dict(dWu=p(4)), I), (dict(dbu=p(9)), I), (dict(dt=2), I), (dict(N=0), I),
         (dict(S=0), I), (dict(M=40000), U), (dict(S=70000), U), (dict(mu=p(12) + 4), A), (dict(dX=p(6) + 2), A), (dict(ws=None), W), (dict(n=64), W)])
 
 
