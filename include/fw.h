@@ -359,9 +359,9 @@ fw_status fw_cond_probe(const float* Phi_y, int M, const float* b0, int k, float
  * (5) Layers of a language model around the whitening: what makes a layer's input rows X [N, M] (one row per token, the rows that
  * fw_cov_accumulate takes as FW_LAYOUT_ROWS), its products, its weight gradients G [S, M], and its answers in 8 bits.  N, M and S
  * need not be multiples of anything; the products copy their operands once to aligned rows where M is not a multiple of 8 (bfloat16)
- * or 16 (8 bits) and the rows are many.  Limits of all of them: N <= 2097152, M <= 32768,
- * S <= 65536.  The workspaces are asked for with
- * d = {N, M, 1, 1, 1, 1, 1, 0, 0}, the geometry of N rows.
+ * or 16 (8 bits) and the rows are many.  Limits of all of them: N <= 2097152, M <= 32768, S <= 65536.  The workspaces are asked for
+ * with d = {N, M, 1, 1, 1, 1, 1, 0, 0}, the geometry of N rows, and for each N that is run: fewer rows may need more, where their
+ * products are cut into runs.
  *
  * Norm by the root mean square of a row, with the residual's addition:
  *   h = X + R (rounded to `dt`: the sum as it is held);   Y = rho h w,   rho = 1 / sqrt(mean_m h^2 + eps)
@@ -403,7 +403,7 @@ fw_status fw_rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float
  *   Z       out  [2, N, S] float32, or NULL: what the backward pass needs of g and u, Z[0] = u act'(g) and Z[1] = act(g).
  *                (The factors rather than g and u, and float32 for both types: a bfloat16 gradient then has two roundings behind it, of
  *                dg or du and its own, 1.4 times the error of its own alone; with g and u in bfloat16 it would be twice that error.)
- *   ws      scratch, fw_workspace_bytes(FW_OP_GATED_FORWARD, M, S, d, dt) bytes
+ *   ws      scratch, fw_workspace_bytes(FW_OP_GATED_FORWARD, M, S, d, dt) bytes (may be 0: then ws may be NULL)
  * Products and sums: FW_BF16 bfloat16 products summed in float32, FW_F32 float32 accuracy.  g, u, the activation and H before its
  * rounding are float32.
  */
