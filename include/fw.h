@@ -372,8 +372,9 @@ fw_status fw_cond_probe(const float* Phi_y, int M, const float* b0, int k, float
  *   H       out  [N, M] element type `dt`: h, or NULL; may be X or R itself
  *   Y       out  [N, M] element type `dt`, or NULL when q is given; overlaps nothing else
  *   q, qs   out  [N, M] 8-bit integers and [N] float32, or both NULL: the same rows in 8 bits, Y ~ qs[n] q[n][m],
- *                qs = max_m |rho h w| / 127, q = the nearest integer (ties to even) to rho h w / qs.  A row of zeros has qs = 0 and
- *                q = 0, a row with an infinite or NaN entry has qs = NaN and q = 0.
+ *                qs = max_m |rho h w| / 127, q = the nearest integer (ties to even) to rho h w / qs, that is to 127 h w / max_m |h w|
+ *                (qs is rounded to float32 as it is stored); a quotient within 2^-47 of a tie counts as one, which without w means a
+ *                tie.  A row of zeros has qs = 0 and q = 0, a row with an infinite or NaN entry has qs = NaN and q = 0.
  * Sums in float64.
  */
 fw_status fw_rms_norm(const void* X, const void* R, fw_dtype dt, int N, int M, const float* w, float eps, void* H, void* Y,
@@ -439,7 +440,7 @@ fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const v
                         const void* dH, const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws,
                         size_t ws_bytes, void* stream);
 
-/* Rows to 8 bits, each with its own scale: qs = max_m |X| / 127, q = the nearest integer (ties to even) to X / qs; zero and
+/* Rows to 8 bits, each with its own scale: qs = max_m |X| / 127, q = the nearest integer (ties to even) to 127 X / max_m |X|; zero and
  * non-finite rows as in fw_rms_norm.  For activations a row is a token, for weights [S, M] a channel.
  *   X  in [N, M] element type `dt`;   q out [N, M];   qs out [N] float32 */
 fw_status fw_int8_rows(const void* X, fw_dtype dt, int N, int M, signed char* q, float* qs, void* stream);

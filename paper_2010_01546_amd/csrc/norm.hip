@@ -7,7 +7,8 @@
 // Bound by memory: each input is read once and each output written once, a row stays in the registers of its group of threads (a
 // wavefront up to 2048 features, a workgroup beyond), 8 entries per lane and access.
 // The sums over a row are float64 (a row of 1e20s has a norm too, and the cost hides behind the loads).  So is q: rho falls out of
-// y / s = 127 h w / max |h w|, whose float32 rounding would put one value in 10^5 on the other side of a half.
+// y / s = 127 h w / max |h w|, whose float32 rounding would put one value in 10^5 on the other side of a half.  127 / top is taken as
+// two numbers (half of a row's largest entry is a tie at 63.5, common in bfloat16; 127 / 158 rounded makes it 63.4999...).
 #include "fw_internal.h"
 #include "lane_sums.h"
 #include <type_traits>
@@ -163,7 +164,8 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void rows_kernel(const T* X, con
     }
     if (!eight) return;
     const bool fine = top > 0.0 && top < __builtin_inf() && rho > 0.0;
-    const double inv = fine ? 127.0 / top : 0.0;
+    // 127 / top as two numbers: v times it, rounded once, is a half where it is one (and, for products with w, within 2^-48 of one)
+    const double inv = fine ? 127.0 / top : 0.0, rest = fine ? fma(-inv, top, 127.0) / top : 0.0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int m = 8 * (t + G * j);
@@ -171,7 +173,10 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void rows_kernel(const T* X, con
         if (!p.any) continue;
         signed char b[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = fine ? (signed char)(int)rint((double)h[j][i] * (double)f[j].v[i] * inv) : (signed char)0;
+        for (int i = 0; i < 8; ++i) {
+            const double v = (double)h[j][i] * (double)f[j].v[i];
+            b[i] = fine ? (signed char)(int)rint(fma(v, inv, v * rest)) : (signed char)0;
+        }
         if (END == WHOLE || j < NV - 1 || (END == RAGGED && p.skip == 0)) {
             __builtin_memcpy(q + at + p.start, b, 8);
         } else {

@@ -1,0 +1,86 @@
+"""GPU parity of the layers around the whitening where a tie, an infinity or a size decides, against the float64 oracle.
+
+Tolerances: U32 = 2^-24 and half(t) (2^-8 for bfloat16, 2^-24 for float32) are the most a rounding is off by, relative to its value."""
+from fractions import Fraction
+
+import numpy as np
+import pytest
+import torch
+
+import workloads as wl
+from gpu_common import DEV, b, dev, relF, workspace
+from oracle import layer_oracle as lo
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+TDT = {"f32": torch.float32, "bf16": torch.bfloat16}
+FDT = {"f32": b.FW_F32, "bf16": b.FW_BF16}
+EPS = 1e-5
+
+
+def nearest_even(v, top):
+    """127 v / top to the nearest integer, ties to even, in whole numbers."""
+    return round(Fraction(127) * v / top)
+
+
+def held(x, dtype):
+    x = np.array([x], dtype=np.float32)
+    return float((wl.round_to_bf16(x) if dtype == "bf16" else x)[0])
+
+
+def step(x, dtype, up):
+    """The next number of the type."""
+    if dtype == "f32":
+        return np.nextafter(np.float32(x), np.float32(np.inf if up else -np.inf))
+    bits = np.float32(x).view(np.uint32) >> 16
+    return np.uint32(int(bits) + (1 if up == (x > 0) else -1) << 16).view(np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ties_of_8_bit_rows(dtype):
+    """Entries halfway between two steps go to the even one, their neighbours to the nearer one: for every bfloat16 significand of the row's
+    largest entry, and (float32) for 24-bit ones, of which the multiples of 127 have ties at every step."""
+    tops = [float(t) for t in range(128, 256)]
+    if dtype == "f32":
+        rng = np.random.default_rng(17)
+        tops += [float(2 * t) for t in rng.integers(1 << 22, 1 << 23, 64)] + [float(254 * t) for t in rng.integers(1 << 13, 1 << 16, 64)]
+    X = np.zeros((len(tops), 268), dtype=np.float32)
+    for row, top in zip(X, tops):
+        halves = [(2 * j + 1) * top / 254 for j in range(127)]
+        halves = [x for x in halves if held(x, dtype) == x and Fraction(x) * 254 % Fraction(top) == 0]
+        assert top / 2 in halves
+        entries = [top] + [s * x for x in halves for s in (1, -1)]
+        entries += [step(s * x, dtype, up) for x in halves[-1:] + [top / 2] for s in (1, -1) for up in (False, True)]
+        row[:len(entries)] = entries
+    N, M = X.shape
+    want = np.array([[nearest_even(Fraction(float(x)), Fraction(t)) for x in row] for row, t in zip(X, tops)])
+    q, qs, q2, qs2 = (torch.zeros(s, dtype=k, device=DEV) for s, k in (((N, M), torch.int8), (N, torch.float32)) * 2)
+    b.fw_int8_rows(dev(X, TDT[dtype]), FDT[dtype], N, M, q, qs)
+    b.fw_rms_norm(dev(X, TDT[dtype]), None, FDT[dtype], N, M, None, EPS, None, None, q2, qs2)
+    torch.cuda.synchronize()
+    assert np.array_equal(q.cpu().numpy(), want)
+    assert np.array_equal(q2.cpu().numpy(), want)
+
+
+def test_ties_of_products_with_the_weights():
+    """h w of 48 bits: halves of the largest one are ties, products a 2^-46th below are not."""
+    rng = np.random.default_rng(18)
+    N, M = 200, 9
+    a = rng.integers(1 << 23, (1 << 24) - 1, N).astype(np.float32)
+    c = np.float32(rng.integers(1 << 23, (1 << 24) - 1)) * np.float32(2.0 ** -24)
+    w = np.full(M, c, dtype=np.float32)
+    w[1:3], w[3], w[4:] = c / 2, np.nextafter(c / 2, np.float32(0)), c / 4
+    X = np.zeros((N, M), dtype=np.float32)
+    X[:, 0], X[:, 1], X[:, 2], X[:, 3] = a, a, -a, a + 1
+    X[:, 3] = np.where((a + 1) * w[3].astype(np.float64) <= a * lo.f64(c), X[:, 3], a)
+    X[:, 4:] = (rng.integers(1, 1 << 24, (N, M - 4)) // 2).astype(np.float32)
+    v = [[Fraction(float(x)) * Fraction(float(y)) for x, y in zip(row, w)] for row in X]
+    top = [max(abs(x) for x in row) for row in v]
+    want = np.array([[nearest_even(x, t) for x in row] for row, t in zip(v, top)])
+    assert (want[:, 1] == 64).all() and (want[:, 2] == -64).all() and (want[:, 3] == 63).any()
+    q, qs = torch.zeros(N, M, dtype=torch.int8, device=DEV), torch.zeros(N, device=DEV)
+    b.fw_rms_norm(dev(X), None, b.FW_F32, N, M, dev(w), EPS, None, None, q, qs)
+    torch.cuda.synchronize()
+    assert np.array_equal(q.cpu().numpy(), want)
