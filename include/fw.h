@@ -433,8 +433,9 @@ fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, cons
  * FW_BF16: dg and du are rounded to bfloat16 for the products (and for mu's part in them) where N S > 524288, below they are held as two
  * bfloat16 numbers each (the rounding would not average out); the sums are float32 and each result is rounded once; dbg and dbu are
  * sums of the values before that rounding.
- * FW_F32: float32 accuracy as in fw_grad_transform's products of three bfloat16 numbers; entries below 2^-110 lose their last bits.  An
- * infinite or NaN entry reaches the results that the formula lets it reach; those are computed once more in float32.
+ * FW_F32: float32 accuracy as in fw_grad_transform's products of three bfloat16 numbers; entries below 2^-110 lose their last bits.
+ * An infinite or NaN entry reaches the results that the formula lets it reach (X - 1 mu^T taken first); those are computed once more in
+ * float32 where the products as they are carried out would give another infinity or NaN.
  */
 fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* Z,
                         const void* dH, const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws,

@@ -142,7 +142,8 @@ template <class T, bool FIX> struct WeightsEpilogue {        // rows below Sp ar
     const float *sums, *mu;               // mu: taken out here (bfloat16), or null
     int S, Sp, M;
     GradInputs<T> in;
-    __device__ __noinline__ floatx4 again(int s, bool up, int m) const {
+    __device__ __noinline__ floatx4 again(int s, bool up, int m) const { return again_here(s, up, m); }
+    __device__ __forceinline__ floatx4 again_here(int s, bool up, int m) const {
         const size_t at = (up ? (size_t)in.N * S : 0) + s;
         const int c = column_of(m, M);
         const float mean = in.mu ? in.mu[c] : 0.f;
@@ -164,6 +165,31 @@ template <class T, bool FIX> struct WeightsEpilogue {        // rows below Sp ar
         if (s >= S || m >= M) return;
         const float out[4] = {v[0], v[1], v[2], v[3]};
         tile_store((r >= Sp ? dWu : dWg) + (size_t)s * M + m, m, M, out);
+    }
+};
+
+// The same in bfloat16 without FIX, with mu: D^T X - (D^T 1) mu^T is inf - inf where the formula has an infinity.  Once a wavefront has stored
+// its results it looks through the sums and the means behind them, and computes those again that come of one which is not finite; each lane
+// stores where it has stored before.  (2048 x 2304 x 6144 with D: 187 us, without this 185; looked for among the results, as FIX does, 201.)
+struct CentredEpilogue : WeightsEpilogue<__bf16, false> {
+    __device__ __forceinline__ void finish(int r0, int rows, int m0, int columns) const {
+        const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+        bool fine = true;
+        for (int i = lane; i < rows; i += 64) fine &= finite(sums[min(r0 + i, 2 * Sp - 1)]);
+        for (int i = lane; i < columns; i += 64) fine &= finite(mu[min(m0 + i, M - 1)]);
+        if (__builtin_amdgcn_ballot_w64(!fine) == 0) return;
+        for (int r = r0 + l16; r - l16 < r0 + rows; r += 16) {
+            const int s = r >= Sp ? r - Sp : r;
+            const float d = sums[min(r, 2 * Sp - 1)];
+            for (int m = m0 + 4 * q; m - 4 * q < m0 + columns; m += 16) {
+                float c[4];
+                tile_vector(mu, m, M, c);
+                const floatx4 v = again_here(min(s, S - 1), r >= Sp, m);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (s < S && m + i < M && !(finite(d) && finite(c[i]))) (r >= Sp ? dWu : dWg)[(size_t)s * M + m + i] = (__bf16)v[i];
+            }
+        }
     }
 };
 
@@ -835,8 +861,11 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
         g.a = bytes(w.D); g.b0 = g.b1 = bytes(X);
         g.apitch = 4ll * Sp; g.bpitch = 2ll * up8(M); g.aplane = N * g.apitch;
         g.partial = w.partial;
-        rc = two ? tile_product<TILE_BF16, true, true, false>(g, WeightsEpilogue<__bf16, true>{dWg, dWu, w.sums, mu, S, Sp, M, in}, st)
-                 : tile_product<TILE_BF16, true, true, false>(g, WeightsEpilogue<__bf16, false>{dWg, dWu, w.sums, mu, S, Sp, M, in}, st);
+        const WeightsEpilogue<__bf16, true> fix = {dWg, dWu, w.sums, mu, S, Sp, M, in};
+        const WeightsEpilogue<__bf16, false> plain = {dWg, dWu, w.sums, mu, S, Sp, M, in};
+        rc = two ? tile_product<TILE_BF16, true, true, false>(g, fix, st)
+             : mu ? tile_product<TILE_BF16, true, true, false>(g, CentredEpilogue{plain}, st)
+                  : tile_product<TILE_BF16, true, true, false>(g, plain, st);
     }
     return rc;
 }

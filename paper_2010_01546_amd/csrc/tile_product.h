@@ -108,6 +108,12 @@ __device__ __forceinline__ void tile_apply(const Epi& epi, int n, int s, const A
     }
 }
 
+// what an epilogue does once a wavefront's results, `rows` from row n and `columns` from column s on, are stored
+template <class Epi> __device__ __forceinline__ auto tile_finish(const Epi& epi, int n, int rows, int s, int columns, int) -> decltype(epi.finish(n, rows, s, columns)) {
+    epi.finish(n, rows, s, columns);
+}
+template <class Epi> __device__ __forceinline__ void tile_finish(const Epi&, int, int, int, int, long) {}
+
 // PAIR: the panel of B holds columns of b0 and the same columns of b1; results tb and tb + WC / 2 of a wavefront belong together.
 template <TileKind KIND, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>
 __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g, Epi epi) {
@@ -377,6 +383,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_product_kernel(TileProduct g,
     const int s = tile_column<WC, PAIR>(J * (PAIR ? 32 : 64) * NCT, wj, lane);
 #pragma unroll
     for (int ta = 0; ta < WR; ++ta) tile_apply<WC, PAIR>(epi, I * 64 * NRT + 16 * (wi * WR + ta) + l16, s, acc[ta]);
+    tile_finish(epi, I * 64 * NRT + 16 * wi * WR, 16 * WR, s - 4 * q, 16 * WC, 0);
 }
 
 // adds the runs of a tile's rows of 16 x 16 results, in order, and applies the epilogue
@@ -402,7 +409,9 @@ __global__ __launch_bounds__(64 * NW) void tile_runs_kernel(TileProduct g, Epi e
             for (int i = 0; i < 4; ++i) acc[tb][i] += v[i];
         }
     }
-    tile_apply<WC, PAIR>(epi, I * 64 * NRT + 16 * (wi * WR + ta) + (lane & 15), tile_column<WC, PAIR>(J * (PAIR ? 32 : 64) * NCT, wj, lane), acc);
+    const int n = I * 64 * NRT + 16 * (wi * WR + ta), s = tile_column<WC, PAIR>(J * (PAIR ? 32 : 64) * NCT, wj, lane);
+    tile_apply<WC, PAIR>(epi, n + (lane & 15), s, acc);
+    tile_finish(epi, n, 16, s - 4 * (lane >> 4), 16 * WC, 0);
 }
 
 // ---- what the epilogues store: four entries of a row from column s on, of `cols`

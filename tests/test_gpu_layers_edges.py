@@ -84,3 +84,34 @@ def test_ties_of_products_with_the_weights():
     b.fw_rms_norm(dev(X), None, b.FW_F32, N, M, dev(w), EPS, None, None, q, qs)
     torch.cuda.synchronize()
     assert np.array_equal(q.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M,S", [(60, 72, 130), (1000, 72, 520), (1030, 72, 520), (1030, 75, 523)])
+def test_infinite_gradients_of_centred_rows(N, M, S, dtype):
+    """With mu, an infinite dg or du makes its row of dWg or dWu infinite with the sign that X - mu has, and NaN where X - mu is zero; in
+    bfloat16 on both sides of the 524288 entries from which on dg and du are one number."""
+    t, dt = TDT[dtype], FDT[dtype]
+    rng = np.random.default_rng(N + M)
+    low = wl.round_to_bf16 if dtype == "bf16" else (lambda x: x)
+    X, Wg, Wu, dH = (low(rng.standard_normal(s).astype(np.float32)) for s in ((N, M), (S, M), (S, M), (N, S)))
+    mu = X.mean(0).astype(np.float32)
+    mu[:5] = 0.0
+    X[3, 7] = mu[7] = 0.25                                       # X - mu = 0 in an infinite row: NaN
+    Z = (0.3 + np.abs(rng.standard_normal((2, N, S)))).astype(np.float32)
+    dH[3, 9], dH[N - 2, S - 1] = np.inf, -np.inf
+    dX, dWg, dWu = (torch.empty(s, dtype=t, device=DEV) for s in ((N, M), (S, M), (S, M)))
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_GRAD, M, S, b.conv_desc(N, M), dt))
+    ws.fill_(255)
+    b.fw_gated_grad(dev(X, t), dt, N, M, S, dev(Wg, t), dev(Wu, t), dev(Z), dev(dH, t), dev(mu), dX, dWg, dWu, None, None, ws)
+    torch.cuda.synchronize()
+    D = [lo.f64(dH) * Z[k] for k in range(2)]
+    with np.errstate(all="ignore"):
+        want = lo.gated_grad_from(D[0], D[1], X, Wg, Wu, mu)
+    for got, w, what in zip((dX, dWg, dWu), want, ("dX", "dWg", "dWu")):
+        got = got.float().cpu().numpy().astype(np.float64)
+        fine = np.isfinite(w)
+        assert np.array_equal(np.isnan(got), np.isnan(w)), what
+        assert np.array_equal(got[np.isinf(w)], w[np.isinf(w)]), what
+        # two roundings to the type, of dg or du and of the result
+        assert fine.any() and relF(got[fine], w[fine]) < (2 * HALF["bf16"] if dtype == "bf16" else 1e-5), what
