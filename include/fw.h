@@ -361,7 +361,8 @@ fw_status fw_cond_probe(const float* Phi_y, int M, const float* b0, int k, float
  * need not be multiples of anything; the products copy their operands once to aligned rows where M is not a multiple of 8 (bfloat16)
  * or 16 (8 bits) and the rows are many.  Limits of all of them: N <= 2097152, M <= 32768, S <= 65536.  The workspaces are asked for
  * with d = {N, M, 1, 1, 1, 1, 1, 0, 0}, the geometry of N rows, and for each N that is run: fewer rows may need more, where their
- * products are cut into runs.
+ * products are cut into runs.  What a call writes, its outputs and its workspace, shares no memory with anything else that it is given;
+ * where an output may be an input, it is the whole of it.  FW_ERR_INVALID_ARG otherwise.
  *
  * Norm by the root mean square of a row, with the residual's addition:
  *   h = X + R (rounded to `dt`: the sum as it is held);   Y = rho h w,   rho = 1 / sqrt(mean_m h^2 + eps)
@@ -370,7 +371,7 @@ fw_status fw_cond_probe(const float* Phi_y, int M, const float* b0, int k, float
  *   w       in   [M] float32, or NULL for all ones
  *   eps     > 0
  *   H       out  [N, M] element type `dt`: h, or NULL; may be X or R itself
- *   Y       out  [N, M] element type `dt`, or NULL when q is given; overlaps nothing else
+ *   Y       out  [N, M] element type `dt`, or NULL when q is given
  *   q, qs   out  [N, M] 8-bit integers and [N] float32, or both NULL: the same rows in 8 bits, Y ~ qs[n] q[n][m],
  *                qs = max_m |rho h w| / 127, q = the nearest integer (ties to even) to rho h w / qs, that is to 127 h w / max_m |h w|
  *                (qs is rounded to float32 as it is stored); a quotient within 2^-47 of a tie counts as one, which without w means a
@@ -429,7 +430,6 @@ fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, cons
  *   dWg, dWu    out  [S, M] element type `dt`, or both NULL
  *   dbg, dbu    out  [S] element type `dt`, or both NULL
  *   ws          scratch, fw_workspace_bytes(FW_OP_GATED_GRAD, M, S, d, dt) bytes
- * The outputs overlap neither each other nor the inputs.
  * FW_BF16: dg and du are rounded to bfloat16 for the products (and for mu's part in them) where N S > 524288, below they are held as two
  * bfloat16 numbers each (the rounding would not average out); the sums are float32 and each result is rounded once; dbg and dbu are
  * sums of the values before that rounding.

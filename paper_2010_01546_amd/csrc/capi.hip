@@ -66,6 +66,26 @@ fw_status rows_check(fw_dtype dt, int N, int M, int S) {
 template <class... P>
 bool all_aligned16(const P*... p) { return (aligned16(p) && ...); }
 
+// The memory of a call: what it writes (outputs and workspace) shares no byte with anything else it is given.  An output that may take an
+// input's place is named once, as an output.
+struct Memory {
+    struct { uintptr_t at; size_t bytes; bool written; } span[16];
+    int n = 0;
+    Memory& add(const void* p, size_t bytes, bool written) {
+        if (p && bytes) span[n++] = {reinterpret_cast<uintptr_t>(p), bytes, written};
+        return *this;
+    }
+    Memory& in(const void* p, size_t bytes) { return add(p, bytes, false); }
+    Memory& out(const void* p, size_t bytes) { return add(p, bytes, true); }
+    bool apart() const {
+        for (int i = 0; i < n; ++i)
+            for (int k = 0; k < i; ++k)
+                if ((span[i].written || span[k].written) && span[i].at < span[k].at + span[k].bytes && span[k].at < span[i].at + span[i].bytes) return false;
+        return true;
+    }
+};
+size_t element(fw_dtype dt) { return dt == FW_BF16 ? 2 : 4; }
+
 }  // namespace
 
 extern "C" {
@@ -314,66 +334,80 @@ fw_status fw_whiten_evd(const float* Phi_x, int M, const fw_evd_params* p, float
 
 fw_status fw_rms_norm(const void* X, const void* R, fw_dtype dt, int N, int M, const float* w, float eps, void* H, void* Y, signed char* q,
                       float* qs, void* stream) {
-    const void* q8 = q;
-    if (!X || (!Y && !q) || !q != !qs || !(eps > 0.f) || (Y && (Y == X || Y == R || Y == H)) || (q && (q8 == X || q8 == R || q8 == H || q8 == Y)))
-        return FW_ERR_INVALID_ARG;
+    if (!X || (!Y && !q) || !q != !qs || !(eps > 0.f)) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, 1);
     if (rc != FW_OK) return rc;
     if (!all_aligned16(X, R, w, H, Y, q, qs)) return FW_ERR_ALIGNMENT;
+    const size_t rows = (size_t)N * M, e = element(dt);
+    if (!Memory().out(H, rows * e).in(X == H ? nullptr : X, rows * e).in(R == H ? nullptr : R, rows * e).in(w, M * sizeof(float)).out(Y, rows * e)
+             .out(q, rows).out(qs, N * sizeof(float)).apart())
+        return FW_ERR_INVALID_ARG;
     return rms_norm(X, R, dt, N, M, w, eps, H, Y, q, qs, reinterpret_cast<hipStream_t>(stream));
 }
 
 fw_status fw_rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float* w, float eps, const void* dY, const void* dH, void* dX,
                            float* dw, void* ws, size_t ws_bytes, void* stream) {
-    if (!H || !dY || (!dX && !dw) || !(eps > 0.f) || dX == H) return FW_ERR_INVALID_ARG;
+    if (!H || !dY || (!dX && !dw) || !(eps > 0.f)) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, 1);
     if (rc != FW_OK) return rc;
     if (!all_aligned16(H, w, dY, dH, dX, dw, ws)) return FW_ERR_ALIGNMENT;
-    if (dw && (!ws || ws_bytes < rms_norm_grad_workspace_bytes(N, M))) return FW_ERR_WORKSPACE;
+    const size_t need = dw ? rms_norm_grad_workspace_bytes(N, M) : 0, rows = (size_t)N * M * element(dt);
+    if (need && (!ws || ws_bytes < need)) return FW_ERR_WORKSPACE;
+    if (!Memory().out(dX, rows).in(H, rows).in(dY == dX ? nullptr : dY, rows).in(dH == dX ? nullptr : dH, rows).in(w, M * sizeof(float))
+             .out(dw, M * sizeof(float)).out(ws, need).apart())
+        return FW_ERR_INVALID_ARG;
     return rms_norm_grad(H, dt, N, M, w, eps, dY, dH, dX, dw, ws, reinterpret_cast<hipStream_t>(stream));
 }
 
 fw_status fw_gated_forward(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu,
                            fw_act act, void* H, float* Z, void* ws, size_t ws_bytes, void* stream) {
-    if (!X || !Wg || !Wu || !H || (int)act < FW_ACT_SILU || (int)act > FW_ACT_RELU || H == X || H == (void*)Z || (Z && (const void*)Z == X)) return FW_ERR_INVALID_ARG;
+    if (!X || !Wg || !Wu || !H || (int)act < FW_ACT_SILU || (int)act > FW_ACT_RELU) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, S);
     if (rc != FW_OK) return rc;
     if (!all_aligned16(X, Wg, Wu, bg, bu, H, Z, ws)) return FW_ERR_ALIGNMENT;
-    const size_t need = gated_forward_workspace_bytes(dt, N, M, S);
+    const size_t need = gated_forward_workspace_bytes(dt, N, M, S), e = element(dt), weights = (size_t)S * M * e, results = (size_t)N * S;
     if (need && (!ws || ws_bytes < need)) return FW_ERR_WORKSPACE;
+    if (!Memory().in(X, (size_t)N * M * e).in(Wg, weights).in(Wu, weights).in(bg, S * sizeof(float)).in(bu, S * sizeof(float)).out(H, results * e)
+             .out(Z, 2 * results * sizeof(float)).out(ws, need).apart())
+        return FW_ERR_INVALID_ARG;
     return gated_forward(X, dt, N, M, S, Wg, Wu, bg, bu, act, H, Z, ws, reinterpret_cast<hipStream_t>(stream));
 }
 
 fw_status fw_gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* Z, const void* dH,
                         const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws, size_t ws_bytes, void* stream) {
     if (!X || !Wg || !Wu || !Z || !dH || !dWg != !dWu || !dbg != !dbu || (!dX && !dWg && !dbg)) return FW_ERR_INVALID_ARG;
-    if (dX && (dX == X || dX == dH || dX == (const void*)Z || dX == Wg || dX == Wu || dX == dWg || dX == dWu)) return FW_ERR_INVALID_ARG;
-    if (dWg && (dWg == dWu || dWg == Wg || dWg == Wu || dWu == Wg || dWu == Wu || dWg == X || dWu == X || dWg == dH || dWu == dH || dWg == (const void*)Z || dWu == (const void*)Z))
-        return FW_ERR_INVALID_ARG;
-    if (dbg && dbg == dbu) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, S);
     if (rc != FW_OK) return rc;
     if (!all_aligned16(X, Wg, Wu, Z, dH, mu, dX, dWg, dWu, dbg, dbu, ws)) return FW_ERR_ALIGNMENT;
-    if (!ws || ws_bytes < gated_grad_workspace_bytes(dt, N, M, S)) return FW_ERR_WORKSPACE;
+    const size_t need = gated_grad_workspace_bytes(dt, N, M, S), e = element(dt), rows = (size_t)N * M * e, weights = (size_t)S * M * e, results = (size_t)N * S;
+    if (!ws || ws_bytes < need) return FW_ERR_WORKSPACE;
+    if (!Memory().in(X, rows).in(Wg, weights).in(Wu, weights).in(Z, 2 * results * sizeof(float)).in(dH, results * e).in(mu, M * sizeof(float))
+             .out(dX, rows).out(dWg, weights).out(dWu, weights).out(dbg, S * e).out(dbu, S * e).out(ws, need).apart())
+        return FW_ERR_INVALID_ARG;
     return gated_grad(X, dt, N, M, S, Wg, Wu, Z, dH, mu, dX, dWg, dWu, dbg, dbu, ws, reinterpret_cast<hipStream_t>(stream));
 }
 
 fw_status fw_int8_rows(const void* X, fw_dtype dt, int N, int M, signed char* q, float* qs, void* stream) {
-    if (!X || !q || !qs || X == (const void*)q) return FW_ERR_INVALID_ARG;
+    if (!X || !q || !qs) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, 1);
     if (rc != FW_OK) return rc;
     if (!all_aligned16(X, q, qs)) return FW_ERR_ALIGNMENT;
+    const size_t rows = (size_t)N * M;
+    if (!Memory().in(X, rows * element(dt)).out(q, rows).out(qs, N * sizeof(float)).apart()) return FW_ERR_INVALID_ARG;
     return int8_rows(X, dt, N, M, q, qs, reinterpret_cast<hipStream_t>(stream));
 }
 
-fw_status fw_int8_product(const signed char* Xq, const float* sx, int N, int M, int S, const signed char* Wq, const float* sw, const float* b,
-                          void* Y, fw_dtype dt, void* ws, size_t ws_bytes, void* stream) {
-    if (!Xq || !sx || !Wq || !sw || !Y || Y == (const void*)Xq || Y == (const void*)Wq) return FW_ERR_INVALID_ARG;
+fw_status fw_int8_product(const signed char* Xq, const float* sx, int N, int M, int S, const signed char* Wq, const float* sw,
+                          const float* b, void* Y, fw_dtype dt, void* ws, size_t ws_bytes, void* stream) {
+    if (!Xq || !sx || !Wq || !sw || !Y) return FW_ERR_INVALID_ARG;
     const fw_status rc = rows_check(dt, N, M, S);
     if (rc != FW_OK) return rc;
     if (!all_aligned16(Xq, sx, Wq, sw, b, Y, ws)) return FW_ERR_ALIGNMENT;
     const size_t need = int8_product_workspace_bytes(N, M, S);
     if (need && (!ws || ws_bytes < need)) return FW_ERR_WORKSPACE;
+    if (!Memory().in(Xq, (size_t)N * M).in(sx, N * sizeof(float)).in(Wq, (size_t)S * M).in(sw, S * sizeof(float)).in(b, S * sizeof(float))
+             .out(Y, (size_t)N * S * element(dt)).out(ws, need).apart())
+        return FW_ERR_INVALID_ARG;
     return int8_product(Xq, sx, N, M, S, Wq, sw, b, Y, dt, ws, reinterpret_cast<hipStream_t>(stream));
 }
 
