@@ -360,8 +360,8 @@ fw_status fw_cond_probe(const float* Phi_y, int M, const float* b0, int k, float
  * fw_cov_accumulate takes as FW_LAYOUT_ROWS), its products, its weight gradients G [S, M], and its answers in 8 bits.  N, M and S
  * need not be multiples of anything; the products copy their operands once to aligned rows where M is not a multiple of 8 (bfloat16)
  * or 16 (8 bits) and the rows are many.  Limits of all of them: N <= 2097152, M <= 32768, S <= 65536.  The workspaces are asked for
- * with d = {N, M, 1, 1, 1, 1, 1, 0, 0}, the geometry of N rows, and for each N that is run: fewer rows may need more, where their
- * products are cut into runs.  What a call writes, its outputs and its workspace, shares no memory with anything else that it is given;
+ * with d = {N, M, 1, 1, 1, 1, 1, 0, 0}, the geometry of N rows; what is given for N rows is enough for any fewer of the same M, S and
+ * type.  What a call writes, its outputs and its workspace, shares no memory with anything else that it is given;
  * where an output may be an input, it is the whole of it.  FW_ERR_INVALID_ARG otherwise.
  *
  * Norm by the root mean square of a row, with the residual's addition:

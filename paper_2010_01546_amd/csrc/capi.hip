@@ -1,5 +1,6 @@
 // C ABI of the feature-whitening library: argument validation, workspace carving, dispatch to the kernels.
 #include "fw_internal.h"
+#include <algorithm>
 
 using namespace fw;
 
@@ -85,6 +86,15 @@ struct Memory {
     }
 };
 size_t element(fw_dtype dt) { return dt == FW_BF16 ? 2 : 4; }
+
+// The most bytes that a number of rows up to N needs.  Between these numbers of rows nothing but the copies of the rows changes, and those
+// grow: the kernels for few rows end at 16, 32 and 64, tiles and runs go by whole 64 rows, and `last` is the last number of rows of a form
+// that needs more for each (0: no such form).  0.3 us for each 64 rows and product.
+template <class F> size_t most_bytes(int N, int last, const F& bytes) {
+    size_t most = bytes(N);
+    for (int n = 16; n < N; n = n < 64 ? 2 * n : n + 64) most = std::max(most, bytes(n));
+    return last > 0 && last < N ? std::max(most, bytes(last)) : most;
+}
 
 }  // namespace
 
@@ -439,9 +449,14 @@ size_t fw_workspace_bytes(fw_op op, int M, int S, const fw_conv_desc* d, fw_dtyp
         case FW_OP_GRAD_TRANSFORM_TAPS:
         case FW_OP_SGD_UPDATE: return (M > 0 && M <= 16384 && S > 0) ? grad_wide_bytes(S, M) + grad_split_bytes(S, M) : 0;
         case FW_OP_RMS_NORM_GRAD: return d && rows_check(dt, d->B, M, 1) == FW_OK ? rms_norm_grad_workspace_bytes(d->B, M) : 0;
-        case FW_OP_GATED_FORWARD: return d && rows_check(dt, d->B, M, S) == FW_OK ? gated_forward_workspace_bytes(dt, d->B, M, S) : 0;
-        case FW_OP_GATED_GRAD: return d && rows_check(dt, d->B, M, S) == FW_OK ? gated_grad_workspace_bytes(dt, d->B, M, S) : 0;
-        case FW_OP_INT8_PRODUCT: return d && rows_check(dt, d->B, M, S) == FW_OK ? int8_product_workspace_bytes(d->B, M, S) : 0;
+        case FW_OP_GATED_FORWARD:
+        case FW_OP_GATED_GRAD:
+        case FW_OP_INT8_PRODUCT:
+            if (!d || rows_check(dt, d->B, M, S) != FW_OK) return 0;
+            return most_bytes(d->B, op == FW_OP_GATED_GRAD ? gated_grad_two_planes_rows(dt, S) : 0, [=](int n) {
+                return op == FW_OP_GATED_FORWARD ? gated_forward_workspace_bytes(dt, n, M, S)
+                       : op == FW_OP_GATED_GRAD  ? gated_grad_workspace_bytes(dt, n, M, S) : int8_product_workspace_bytes(n, M, S);
+            });
         case FW_OP_DIAGNOSTICS: return M > 0 && M <= 16384 ? diagnostics_workspace_bytes(M) : 0;
         case FW_OP_COND_PROBE: return M > 0 && M <= 16384 ? cond_probe_workspace_bytes(M, S > 0 ? S : FW_COND_PROBE_MAX_K) : 0;
     }

@@ -198,6 +198,7 @@ fw_status int8_rows(const void* X, fw_dtype dt, int N, int M, signed char* q, fl
 // ---- gated.hip
 size_t gated_forward_workspace_bytes(fw_dtype dt, int N, int M, int S);
 size_t gated_grad_workspace_bytes(fw_dtype dt, int N, int M, int S);
+int gated_grad_two_planes_rows(fw_dtype dt, int S);      // the most rows whose dg and du are held as two bfloat16 numbers each
 fw_status gated_forward(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu,
                         fw_act act, void* H, float* Z, void* ws, hipStream_t st);
 fw_status gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* Z, const void* dH,

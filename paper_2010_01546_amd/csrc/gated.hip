@@ -583,7 +583,8 @@ inline int up64(int s) { return (s + 63) / 64 * 64; }
 // bfloat16: D in two planes, 16 bits, where the rounding to 8 bits does not average out: it adds an error as large as that of rounding the
 // result, 1.42 times the latter together, but up to 1.8 times where a few entries make up the sum (11 x 64, S = 64).  The products then
 // go over the weights twice; small ones are bound by their launches.
-inline bool two_planes(fw_dtype dt, int N, int S) { return dt == FW_BF16 && (long long)N * S <= 1 << 19; }
+constexpr int kTwoPlanes = 1 << 19;
+inline bool two_planes(fw_dtype dt, int N, int S) { return dt == FW_BF16 && (long long)N * S <= kTwoPlanes; }
 // rows of a workgroup of gate_grad_kernel: 64, or 16 where that leaves compute units without work (777 x 1001: 13.9 us with 64)
 inline int grad_rows(int N, int S) { return (long long)((N + 63) / 64) * ((S + 255) / 256) >= 1024 ? 64 : 16; }
 inline int row_blocks(int N, int S) { return (up64(N) + grad_rows(N, S) - 1) / grad_rows(N, S); }
@@ -874,6 +875,7 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
 
 size_t gated_forward_workspace_bytes(fw_dtype dt, int N, int M, int S) { return forward_ws(dt, N, M, S, nullptr).total; }
 size_t gated_grad_workspace_bytes(fw_dtype dt, int N, int M, int S) { return grad_ws(dt, N, M, S, nullptr).total; }
+int gated_grad_two_planes_rows(fw_dtype dt, int S) { return dt == FW_BF16 ? kTwoPlanes / S : 0; }
 
 fw_status gated_forward(const void* X, fw_dtype dt, int N, int M, int S, const void* Wg, const void* Wu, const float* bg, const float* bu,
                         fw_act act, void* H, float* Z, void* ws, hipStream_t st) {

@@ -115,3 +115,30 @@ def test_infinite_gradients_of_centred_rows(N, M, S, dtype):
         assert np.array_equal(got[np.isinf(w)], w[np.isinf(w)]), what
         # two roundings to the type, of dg or du and of the result
         assert fine.any() and relF(got[fine], w[fine]) < (2 * HALF["bf16"] if dtype == "bf16" else 1e-5), what
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_one_workspace_for_all_numbers_of_rows(dtype):
+    """A workspace of the largest batch, as a program keeps it: smaller ones run in it and give what they give in their own."""
+    most, M, S, t, dt = 1500, 580, 900, TDT[dtype], FDT[dtype]
+    rng = np.random.default_rng(3)
+    X, Wg, Wu, dH = (dev(rng.standard_normal(s).astype(np.float32) / 8, t) for s in ((most, M), (S, M), (S, M), (most, S)))
+    Xq, Wq = (dev(rng.integers(-127, 128, s), torch.int8) for s in ((most, M), (S, M)))
+    scale = torch.ones(most, device=DEV)
+    ops = (b.FW_OP_GATED_FORWARD, b.FW_OP_GATED_GRAD, b.FW_OP_RMS_NORM_GRAD, b.FW_OP_INT8_PRODUCT)
+    space = lambda N: [torch.full((b.fw_workspace_bytes(op, M, S, b.conv_desc(N, M), dt),), 255, dtype=torch.uint8, device=DEV) for op in ops]  # noqa: E731
+
+    def run(N, ws):
+        H, Z, dX, dY = (torch.empty(s, dtype=k, device=DEV) for s, k in (((N, S), t), ((2, N, S), torch.float32), ((N, M), t), ((N, M), t)))
+        dWg, dWu, dw, Y = (torch.empty(s, dtype=k, device=DEV) for s, k in (((S, M), t), ((S, M), t), ((M,), torch.float32), ((N, S), t)))
+        b.fw_gated_forward(X, dt, N, M, S, Wg, Wu, None, None, b.FW_ACT_SILU, H, Z, ws[0])
+        b.fw_gated_grad(X, dt, N, M, S, Wg, Wu, Z, dH, None, dX, dWg, dWu, None, None, ws[1])
+        b.fw_rms_norm_grad(X, dt, N, M, None, EPS, dX, None, dY, dw, ws[2])
+        b.fw_int8_product(Xq, scale, N, M, S, Wq, scale, None, Y, dt, ws[3])
+        torch.cuda.synchronize()
+        return H, Z, dX, dY, dWg, dWu, dw, Y
+
+    kept = space(most)
+    for N in (most, 1, 16, 17, 40, 64, 65, 200, (1 << 19) // S, (1 << 19) // S + 1, 700, 1024, 1499):
+        for a, c in zip(run(N, kept), run(N, space(N))):
+            assert torch.equal(a, c), N

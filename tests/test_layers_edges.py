@@ -53,3 +53,14 @@ def test_shared_memory_is_refused(name, dt):
                 assert call(*args) == b.FW_ERR_INVALID_ARG, (out, other, shift)
                 seen += 1
     assert seen > 5
+
+
+@pytest.mark.parametrize("dt", [b.FW_F32, b.FW_BF16])
+@pytest.mark.parametrize("op", [b.FW_OP_RMS_NORM_GRAD, b.FW_OP_GATED_FORWARD, b.FW_OP_GATED_GRAD, b.FW_OP_INT8_PRODUCT])
+@pytest.mark.parametrize("M,S", [(64, 64), (33, 700), (576, 2304), (1153, 1001), (4608, 12288), (4609, 521)])
+def test_a_workspace_is_enough_for_fewer_rows(M, S, op, dt):
+    """No size is smaller than that of fewer rows; single rows around where forms change, odd steps between."""
+    near = lambda n: range(max(1, n - 3), n + 4)  # noqa: E731
+    N = sorted({*range(1, 140), *range(140, 9000, 37), *near(8192), *near((1 << 19) // S), *near(4096), *(64 * k + j for k in range(1, 40) for j in (0, 1))})
+    sizes = [b.fw_workspace_bytes(op, M, S, b.conv_desc(n, M), dt) for n in N]
+    assert all(x <= y for x, y in zip(sizes, sizes[1:]))
