@@ -21,6 +21,10 @@ template <class T> struct ScaleEpilogue {
         const float x = sx[n];
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = (float)acc[i] * x * w[i] + c[i];
+        if (fabsf(x) > 0x1p96f) {             // a sum of up to 2^30 times x may leave float32 on the way to a result that is inside it
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = (float)acc[i] * (x * 0x1p-40f) * w[i] * 0x1p40f + c[i];
+        }
         tile_store(Y + (size_t)n * S + s, s, S, y);
     }
 };

@@ -142,3 +142,23 @@ def test_one_workspace_for_all_numbers_of_rows(dtype):
     for N in (most, 1, 16, 17, 40, 64, 65, 200, (1 << 19) // S, (1 << 19) // S + 1, 700, 1024, 1499):
         for a, c in zip(run(N, kept), run(N, space(N))):
             assert torch.equal(a, c), N
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,M,S", [(5, 64, 70), (200, 144, 300)])
+def test_scales_far_from_one(N, M, S, dtype):
+    """A sum times its token's scale may lie outside float32 where the result does not."""
+    rng = np.random.default_rng(N)
+    Xq, Wq = rng.integers(-127, 128, (N, M)).astype(np.int8), rng.integers(-127, 128, (S, M)).astype(np.int8)
+    sx = (np.exp(rng.standard_normal(N)) * np.where(np.arange(N) % 2, 1e36, 1e-36)).astype(np.float32)
+    sw = (np.exp(rng.standard_normal(S)) * np.where(np.arange(S) % 3, 1e-7, 1e-30)).astype(np.float32)
+    Xq[0] = 0                                                    # 0 times anything finite
+    Y = torch.empty(N, S, dtype=TDT[dtype], device=DEV)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_INT8_PRODUCT, M, S, b.conv_desc(N, M), FDT[dtype]))
+    b.fw_int8_product(dev(Xq, torch.int8), dev(sx), N, M, S, dev(Wq, torch.int8), dev(sw), None, Y, FDT[dtype], ws)
+    torch.cuda.synchronize()
+    want = lo.int8_product(Xq, sx, Wq, sw)
+    got = Y.float().cpu().numpy().astype(np.float64)
+    assert np.abs(want).max() < 3e38 and np.isfinite(got).all()
+    # the sum's and both products' roundings and the type's; below 2^-126 a float32 number is off by up to 2^-150
+    assert (np.abs(got - want) <= 4 * U32 * np.abs(want) + HALF[dtype] * np.abs(want) + 2.0 ** -133).all()
