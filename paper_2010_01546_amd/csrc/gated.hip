@@ -644,7 +644,7 @@ TileProduct weights_plan(fw_dtype dt, int N, int M, int S) {
     TileProduct g = {};
     g.R = 2 * up64(S); g.C = M; g.klen = N;
     g.part = g.once = (N + 63) / 64; g.stages = two_planes(dt, N, S) ? 2 * g.once : g.once;
-    tile_plan(g, false, dt == FW_F32, dt == FW_F32 ? 4 : 2);
+    tile_plan(g, false, dt == FW_F32, dt == FW_F32 ? 4 : 2, true);
     return g;
 }
 

@@ -446,10 +446,13 @@ __device__ __forceinline__ void tile_vector(const float* p, int s, int cols, flo
 // Runs are for the tiles behind whole rounds, and keep at least 4 stages (of planes: 2, each with six products).
 // The constants are fitted to 123 products (20 to 8192 rows, 64 to 12288 columns and features) with every shape and number of runs
 // measured: what is chosen takes 0.5 % longer than the best on average, 8 % at most.
-inline void tile_plan(TileProduct& g, bool pair, bool planes, double bytes) {
+// even: an even number of 64 rows (both weights' gradients below each other), of which 64 x 256 results never beat 128 x 128: as many
+// tiles or more, longer loads.
+inline void tile_plan(TileProduct& g, bool pair, bool planes, double bytes, bool even = false) {
     static const int shapes[][2] = {{4, 4}, {2, 4}, {2, 2}, {1, 4}, {1, 2}};
     double best = 1e300;
     for (int i = planes ? 1 : 0; i < 5; ++i) {               // the planes of 256 x 256 results do not fit into LDS
+        if (even && i == 3) continue;
         const int nrt = shapes[i][0], nct = shapes[i][1], tc = pair ? 32 * nct : 64 * nct;
         const int nrb = (g.R + 64 * nrt - 1) / (64 * nrt), ncb = (g.C + tc - 1) / tc;
         const long long tiles = (long long)nrb * ncb;
@@ -491,7 +494,8 @@ fw_status tile_product(const TileProduct& g, const Epi& epi, hipStream_t st) {
         if (g.nrt == 4) return tile_launch<KIND, 4, 4, 8, AKM, BKM, PAIR>(g, epi, st);
     if (g.nrt == 2 && g.nct == 4) return tile_launch<KIND, 2, 4, 8, AKM, BKM, PAIR>(g, epi, st);
     if (g.nrt == 2) return tile_launch<KIND, 2, 2, 8, AKM, BKM, PAIR>(g, epi, st);
-    if (g.nct == 4) return tile_launch<KIND, 1, 4, 8, AKM, BKM, PAIR>(g, epi, st);
+    if constexpr (!AKM)                                      // the rows are outputs of both weights: an even number of 64 (tile_plan)
+        if (g.nct == 4) return tile_launch<KIND, 1, 4, 8, AKM, BKM, PAIR>(g, epi, st);
     return tile_launch<KIND, 1, 2, 8, AKM, BKM, PAIR>(g, epi, st);
 }
 
