@@ -195,7 +195,16 @@ fw_status rms_norm_grad(const void* H, fw_dtype dt, int N, int M, const float* w
                         float* dw, void* ws, hipStream_t st);
 fw_status int8_rows(const void* X, fw_dtype dt, int N, int M, signed char* q, float* qs, hipStream_t st);
 
+// How a matrix-core product of the layers is cut, for tests of every way; no caller of the library has to know.
+struct TileChoice {
+    int few;                 // few rows: no tiles, the fields below are zero
+    int rows, columns;       // of a tile
+    int whole, cut, runs;    // tiles with the whole contraction, tiles cut into `runs`
+    int stages;              // of 128 bytes of the contraction
+};
+
 // ---- gated.hip
+void gated_tiles(int product, fw_dtype dt, int N, int M, int S, TileChoice* c);      // product: 0 projections, 1 dX, 2 dWg and dWu
 size_t gated_forward_workspace_bytes(fw_dtype dt, int N, int M, int S);
 size_t gated_grad_workspace_bytes(fw_dtype dt, int N, int M, int S);
 int gated_grad_two_planes_rows(fw_dtype dt, int S);      // the most rows whose dg and du are held as two bfloat16 numbers each
@@ -205,6 +214,7 @@ fw_status gated_grad(const void* X, fw_dtype dt, int N, int M, int S, const void
                      const float* mu, void* dX, void* dWg, void* dWu, void* dbg, void* dbu, void* ws, hipStream_t st);
 
 // ---- int8.hip
+void int8_tiles(int N, int M, int S, TileChoice* c);
 size_t int8_product_workspace_bytes(int N, int M, int S);
 fw_status int8_product(const signed char* Xq, const float* sx, int N, int M, int S, const signed char* Wq, const float* sw, const float* b,
                        void* Y, fw_dtype dt, void* ws, hipStream_t st);

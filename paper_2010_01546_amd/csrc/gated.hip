@@ -873,6 +873,10 @@ fw_status grad_bf16(const void* X, int N, int M, int S, const void* Wg, const vo
 
 }  // namespace
 
+void gated_tiles(int product, fw_dtype dt, int N, int M, int S, TileChoice* c) {
+    if (product == 0 ? few_forward(dt, N, M, S) : few_grad(dt, N, M, S)) *c = {1};
+    else *c = tile_choice(product == 0 ? forward_plan(dt, N, M, S) : product == 1 ? rows_plan(dt, N, M, S) : weights_plan(dt, N, M, S), product == 0);
+}
 size_t gated_forward_workspace_bytes(fw_dtype dt, int N, int M, int S) { return forward_ws(dt, N, M, S, nullptr).total; }
 size_t gated_grad_workspace_bytes(fw_dtype dt, int N, int M, int S) { return grad_ws(dt, N, M, S, nullptr).total; }
 int gated_grad_two_planes_rows(fw_dtype dt, int S) { return dt == FW_BF16 ? kTwoPlanes / S : 0; }

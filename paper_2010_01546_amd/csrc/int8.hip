@@ -66,6 +66,11 @@ size_t padded_bytes(int R, int M) { return M % 16 ? align_up((size_t)R * up16(M)
 
 }  // namespace
 
+void int8_tiles(int N, int M, int S, TileChoice* c) {
+    if (few_rows(N, S, M % 16 == 0, false)) *c = {1};
+    else *c = tile_choice(plan(N, M, S), false);
+}
+
 size_t int8_product_workspace_bytes(int N, int M, int S) {
     if (few_rows(N, S, M % 16 == 0, false)) return 0;
     return padded_bytes(N, M) + padded_bytes(S, M) + tile_partial_bytes(plan(N, M, S));

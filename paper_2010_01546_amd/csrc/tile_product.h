@@ -473,6 +473,9 @@ inline void tile_plan(TileProduct& g, bool pair, bool planes, double bytes, bool
         }
     }
 }
+inline TileChoice tile_choice(const TileProduct& g, bool pair) {
+    return {0, 64 * g.nrt, (pair ? 32 : 64) * g.nct, g.full, g.rest, g.runs, g.stages};
+}
 inline size_t tile_partial_bytes(const TileProduct& g) { return align_up((size_t)g.rest * g.runs * g.nrt * g.nct * 16384, 256); }
 
 template <TileKind KIND, int NRT, int NCT, int NW, bool AKM, bool BKM, bool PAIR, class Epi>

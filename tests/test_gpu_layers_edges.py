@@ -7,9 +7,11 @@ import numpy as np
 import pytest
 import torch
 
+import layer_tiles as tiles
 import workloads as wl
 from gpu_common import DEV, b, dev, relF, workspace
 from oracle import layer_oracle as lo
+from test_gpu_layers import Out
 
 pytestmark = pytest.mark.gpu
 
@@ -162,3 +164,91 @@ def test_scales_far_from_one(N, M, S, dtype):
     assert np.abs(want).max() < 3e38 and np.isfinite(got).all()
     # the sum's and both products' roundings and the type's; below 2^-126 a float32 number is off by up to 2^-150
     assert (np.abs(got - want) <= 4 * U32 * np.abs(want) + HALF[dtype] * np.abs(want) + 2.0 ** -133).all()
+
+
+# ------------------------------------------------------------------------------- every tile and cut, all results, in float64 on the GPU
+
+def within(got, want, tol, what):
+    bad = ~((got.double() - want).abs() <= tol)
+    if bool(bad.any()):
+        i = tuple(bad.nonzero()[0].tolist())
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} off, first at {i}: {got[i].item()!r} for {want[i].item()!r}, allowed {tol[i].item():.3g}")
+
+
+def close(got, want, roundings, what):
+    """float32, as a whole: the roundings of a sum of K terms of either sign are each at most U32 of a partial sum, which is no larger than
+    the whole one in the mean of squares, and of either sign, so that sqrt(K) of them remain.  (One of six products of the three
+    planes left out is 2^-18.)"""
+    rel = (torch.linalg.vector_norm(got.double() - want) / torch.linalg.vector_norm(want)).item()
+    assert rel < roundings * U32, (what, rel, roundings * U32)
+
+
+def untouched(*outs):
+    for x in outs:
+        tail = x.buf[x.t.numel():].float()
+        assert bool((tail == 77).all() if x.fill == 77 else torch.isnan(tail).all()), "written behind the end"
+
+
+@pytest.mark.parametrize("dtype,N,M,S", [("bf16", *s) for s in tiles.BF16_SIZES] + [("f32", *s) for s in tiles.F32_SIZES])
+def test_gated_block_of_every_tile(dtype, N, M, S):
+    t, dt, half = TDT[dtype], FDT[dtype], HALF[dtype]
+    gen = torch.Generator(device=DEV).manual_seed(N + M + S)
+    new = lambda *s, scale=1.0: scale * torch.randn(*s, generator=gen, device=DEV)  # noqa: E731
+    X = (new(N, M) * torch.exp(0.5 * new(M))).to(t)
+    Wg, Wu, dH = (new(*s, scale=c).to(t) for s, c in (((S, M), M ** -0.5), ((S, M), M ** -0.5), ((N, S), 0.1)))
+    bg, bu = new(S, scale=0.3), new(S, scale=0.3)
+    mu = X.float().mean(0) + 0.1 if (N + M) % 4 else None
+    H, Z = Out(N, S, dtype=t), Out(2, N, S, dtype=torch.float32)
+    dX, dWg, dWu, dbg, dbu = (Out(*s, dtype=t) for s in ((N, M), (S, M), (S, M), (S,), (S,)))
+    d = b.conv_desc(N, M)
+    ws = [torch.full((max(b.fw_workspace_bytes(op, M, S, d, dt), 16),), 255, dtype=torch.uint8, device=DEV) for op in (b.FW_OP_GATED_FORWARD, b.FW_OP_GATED_GRAD)]
+    b.fw_gated_forward(X, dt, N, M, S, Wg, Wu, bg, bu, b.FW_ACT_SILU, H.t, Z.t, ws[0])
+    b.fw_gated_grad(X, dt, N, M, S, Wg, Wu, Z.t, dH, mu, dX.t, dWg.t, dWu.t, dbg.t, dbu.t, ws[1])
+    torch.cuda.synchronize()
+    untouched(H, Z, dX, dWg, dWu, dbg, dbu)
+    x, wg, wu = X.double(), Wg.double(), Wu.double()
+    g, u = x @ wg.T + bg, x @ wu.T + bu
+    # a sum of K terms in float32, in any order, is off by (K + a few) U32 of the terms' magnitudes; slopes of silu and of its slope are
+    # below 1.2; the activation is off by a few units of float32 of max(|g|, 1)
+    eg, eu = ((M + 8) * U32 * (x.abs() @ w.abs().T + c.abs()) for w, c in ((wg, bg), (wu, bu)))
+    p = torch.sigmoid(g)
+    a, da = g * p, p + g * p * (1 - p)
+    within(H.t, a * u, 1.2 * eg * (u.abs() + eu) + a.abs() * eu + 16 * U32 * (g * u).abs() + (a * u).abs() * half + 1e-38, "H")
+    within(Z.t[0], u * da, 1.2 * eg * u.abs() + 1.2 * eu + 16 * U32 * (1 + g.abs()) * u.abs() + 1e-38, "Z[0]")
+    within(Z.t[1], a, 1.2 * eg + 16 * U32 * g.abs() + 1e-38, "Z[1]")
+    if dtype == "f32":       # slope 1.2 of an activation half as large in the mean of squares, and the other factor's own error
+        close(H.t, a * u, 4 * M ** 0.5 + 32, "H")
+        close(Z.t[1], a, 3 * M ** 0.5 + 32, "Z[1]")
+    del g, u, p, a, da, eg, eu
+    # the gradients of what was kept: dg and du in float32, in bfloat16 rounded to one number where there are many, to two otherwise
+    one = dtype == "bf16" and N * S > 1 << 19
+    more = U32 if dtype == "f32" else 0.0 if one else U32 + 2.0 ** -16
+    D = [dH.float() * Z.t[k] for k in range(2)]
+    for got, v, what in ((dbg, D[0], "dbg"), (dbu, D[1], "dbu")):
+        within(got.t, v.double().sum(0), (N + 5) * U32 * v.double().abs().sum(0) + half * v.double().sum(0).abs(), what)
+    D = [v.to(t).double() if one else v.double() for v in D]
+    want = D[0] @ wg + D[1] @ wu
+    within(dX.t, want, ((2 * S + 8) * U32 + more) * (D[0].abs() @ wg.abs() + D[1].abs() @ wu.abs()) + half * want.abs(), "dX")
+    if dtype == "f32":
+        close(dX.t, want, (2 * S) ** 0.5 + 8, "dX")
+    xc, xm = (x, x.abs()) if mu is None else (x - mu, x.abs() + mu.abs())
+    for got, v, what in ((dWg, D[0], "dWg"), (dWu, D[1], "dWu")):
+        want = v.T.contiguous() @ xc
+        within(got.t, want, ((2 * N + 8) * U32 + more) * (v.abs().T.contiguous() @ xm.double()) + half * want.abs(), what)
+        if dtype == "f32":
+            close(got.t, want, N ** 0.5 + 8, what)
+
+
+@pytest.mark.parametrize("N,M,S", tiles.INT8_SIZES)
+def test_int8_product_of_every_tile(N, M, S):
+    gen = torch.Generator(device=DEV).manual_seed(N + M + S)
+    Xq, Wq = (torch.randint(-127, 128, s, generator=gen, device=DEV, dtype=torch.int8) for s in ((N, M), (S, M)))
+    sx, sw = (torch.exp(torch.randn(n, generator=gen, device=DEV)) for n in (N, S))
+    bias = torch.randn(S, generator=gen, device=DEV)
+    Y = Out(N, S, dtype=torch.float32)
+    ws = torch.full((max(b.fw_workspace_bytes(b.FW_OP_INT8_PRODUCT, M, S, b.conv_desc(N, M), b.FW_F32), 16),), 255, dtype=torch.uint8, device=DEV)
+    b.fw_int8_product(Xq, sx, N, M, S, Wq, sw, bias, Y.t, b.FW_F32, ws)
+    torch.cuda.synchronize()
+    untouched(Y)
+    plain = (Xq.double() @ Wq.double().T) * sx.double()[:, None] * sw.double()
+    within(Y.t, plain + bias, 4 * U32 * (plain.abs() + bias.abs()), "Y")

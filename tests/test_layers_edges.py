@@ -1,6 +1,7 @@
 """Layers around the whitening, host side: memory that a call must not share, workspaces over all numbers of rows (no kernel runs)."""
 import pytest
 
+import layer_tiles as tiles
 from paper_2010_01546_amd import binding as b
 
 BASE, GAP = 1 << 20, 1 << 24          # aligned, never dereferenced: validation fails first
@@ -64,3 +65,24 @@ def test_a_workspace_is_enough_for_fewer_rows(M, S, op, dt):
     N = sorted({*range(1, 140), *range(140, 9000, 37), *near(8192), *near((1 << 19) // S), *near(4096), *(64 * k + j for k in range(1, 40) for j in (0, 1))})
     sizes = [b.fw_workspace_bytes(op, M, S, b.conv_desc(n, M), dt) for n in N]
     assert all(x <= y for x, y in zip(sizes, sizes[1:]))
+
+
+def test_sizes_reach_every_tile_and_cut():
+    """What the tests on the GPU compare in full: every shape that a product is given, whole, cut into runs, and whole rounds with a cut rest
+    behind them.  256 x 256 results (projections: 128 columns of both) are for two-byte and one-byte operands."""
+    cuts = ("whole", "runs", "both")
+    gates, plain = ("64x64", "64x128", "128x64", "128x128"), ("64x128", "64x256", "128x128", "128x256")
+    for dt, sizes, largest in ((b.FW_BF16, tiles.BF16_SIZES, "256x256"), (b.FW_F32, tiles.F32_SIZES, None)):
+        for product in ("forward", "dX", "dW"):
+            shapes = list(gates if product == "forward" else plain) + ([largest.replace("x256", "x128") if product == "forward" else largest] if largest else [])
+            if product == "dW":
+                shapes.remove("64x256")                  # its rows are an even number of 64
+            got = {tiles.way(tiles.choice(product, dt, *s)) for s in sizes}
+            assert got - {None} == {(s, c) for s in shapes for c in cuts}, (dt, product)
+    got = {tiles.way(tiles.choice("int8", b.FW_F32, *s)) for s in tiles.INT8_SIZES}
+    assert got - {None} == {(s, c) for s in plain + ("256x256",) for c in cuts}
+
+
+def test_few_rows_take_no_tiles():
+    assert tiles.choice("forward", b.FW_F32, 32, 576, 200).few and tiles.choice("dW", b.FW_F32, 32, 576, 200).few and tiles.choice("int8", b.FW_F32, 16, 576, 200).few
+    assert not tiles.choice("forward", b.FW_F32, 65, 576, 200).few and not tiles.choice("dX", b.FW_BF16, 1, 576, 200).few
