@@ -8,8 +8,9 @@
 // products of it: dX = D [Wg; Wu], whose contraction runs over the rows of both weight matrices, and [dWg; dWu] = D^T X.  Operands that
 // are contraction-major in memory are turned on the way out of LDS, not in memory.  mu is taken out of the sums: D^T (X - 1 mu^T) =
 // D^T X - (D^T 1) mu^T, with D^T 1 summed from D as it is held, so that the identity is exact but for float32 sums.
-// 8192 x 4608 to 12288: projections 1470 us (1.26 PFLOP/s; 140 more with Z), D 275 (the rate of HBM), dX 1284 (1.45), dWg and dWu 1326 (1.40):
-// the power limit.
+// 8192 x 4608 to 12288, each launch as a pass of all of them has it: projections 1650 to 1780 us (Z stored; alone and without Z 1290, 1.44 PFLOP/s),
+// D 291 to 300 (the rate of HBM), dX 1250 to 1530 (1.2 to 1.48 PFLOP/s), dWg and dWu 1350 to 1850 (1.0 to 1.37): the power limit, lower ends
+// after a few passes.
 // float32: the same products with every operand as three bfloat16 planes (tile_product.h), split in one pass over X and the weights, D
 // when it is formed.  X is centred on mu as it is split.
 // float32 with few rows: float32 matrix instructions on the operands as they are (few_product_kernel, few_rows_grad_kernel,
@@ -582,7 +583,9 @@ inline int up8(int m) { return (m + 7) / 8 * 8; }
 inline int up64(int s) { return (s + 63) / 64 * 64; }
 // bfloat16: D in two planes, 16 bits, where the rounding to 8 bits does not average out: it adds an error as large as that of rounding the
 // result, 1.42 times the latter together, but up to 1.8 times where a few entries make up the sum (11 x 64, S = 64).  The products then
-// go over the weights twice; small ones are bound by their launches.
+// go over X or the weights twice, and their epilogue looks for results that are not finite: next to nothing where launches bound them, but
+// large weights have few rows on this side too (4608 features, 12288: 42 rows in two planes dX 89 us, dWg and dWu 149; 43 rows in one 58 and
+// 96; 576 to 2304: 227 rows 30 and 24, 228 rows 21 and 16).
 constexpr int kTwoPlanes = 1 << 19;
 inline bool two_planes(fw_dtype dt, int N, int S) { return dt == FW_BF16 && (long long)N * S <= kTwoPlanes; }
 // rows of a workgroup of gate_grad_kernel: 64, or 16 where that leaves compute units without work (777 x 1001: 13.9 us with 64)

@@ -1,6 +1,7 @@
 // Product of rows in 8 bits with weights in 8 bits, a scale per token and per channel:
 //   Y[n][s] = sx[n] sw[s] sum_m Xq[n][m] Wq[s][m] + b[s],   the sums exact in 32-bit integers (tile_product.h)
-// 8192 x 4608 to 12288: 421 to 436 us (2.1 to 2.2 POP/s, the power limit); 16 x 12288 to 4608: 11.6 us (4.9 TB/s).
+// 8192 x 4608 to 12288: 421 to 457 us by card and pass (2.0 to 2.2 POP/s, the power limit); 16 x 12288 to 4608: 14.7 us from HBM (3.8 TB/s),
+// 11.6 with the weights in the last-level cache.
 #include "fw_internal.h"
 #include "tile_product.h"
 

@@ -3,7 +3,8 @@
 //   h = x + r,  rho = 1 / sqrt(mean h^2 + eps),  y = rho h w;      8 bits: s = max |y| / 127, q = rint(y / s)
 //   dx = rho w dy - h rho^3 / M sum(w dy h) + dh,                  dw = sum over rows of dy h rho
 //
-// 8192 x 4608 bfloat16 with residual: norm 56.8 us (5.3 TB/s), gradient 72 us (4.2 TB/s; 5 of it the sum over the workgroups' dw).
+// 8192 x 4608 bfloat16 with residual: norm 57 us a pass among others (5.3 TB/s), gradient 72 (4.2 TB/s); the kernels by themselves, after
+// other work, 50 and 66 + 5 (the sum over the workgroups' dw).
 // Bound by memory: each input is read once and each output written once, a row stays in the registers of its group of threads (a
 // wavefront up to 2048 features, a workgroup beyond), 8 entries per lane and access.
 // The sums over a row are float64 (a row of 1e20s has a norm too, and the cost hides behind the loads).  So is q: rho falls out of

@@ -445,7 +445,8 @@ __device__ __forceinline__ void tile_vector(const float* p, int s, int cols, flo
 // instructions and its loads + the first loads + storing the results, `bytes` each), plus the launch that adds the runs and its traffic.
 // Runs are for the tiles behind whole rounds, and keep at least 4 stages (of planes: 2, each with six products).
 // The constants are fitted to 123 products (20 to 8192 rows, 64 to 12288 columns and features) with every shape and number of runs
-// measured: what is chosen takes 0.5 % longer than the best on average, 8 % at most.
+// measured: what is chosen takes 0.5 % longer than the best on average, 8 % at most.  The projections among them stored Z; without it they
+// are planned alike, though they store a third to a fifth (501 x 2304 x 6145: 42 us without, 52 with).
 // even: an even number of 64 rows (both weights' gradients below each other), of which 64 x 256 results never beat 128 x 128: as many
 // tiles or more, longer loads.
 inline void tile_plan(TileProduct& g, bool pair, bool planes, double bytes, bool even = false) {
@@ -507,8 +508,9 @@ fw_status tile_product(const TileProduct& g, const Epi& epi, hipStream_t st) {
 // A workgroup owns `cols` columns (PAIR: of each matrix), so many that every compute unit gets as much of B to read; its wavefronts take
 // stages of 128 bytes in turn, two ahead in registers, turn them through LDS of their own (eight lanes load the 128 bytes of a
 // row, so that whole cache lines are asked for) and add up their sums at the end: one launch, no workspace, no padded copies.
-// Two projections of one row of 4608 bfloat16, 12288 columns: 42.7 us, 5.3 TB/s; 16 rows of 12288 bytes, 4608 columns: 11.6 us, 4.9 TB/s.
-// (Tiles of 64 rows whose contraction is cut into runs: 43.7 and 18.0 us; 1 x 1153, 1001 columns, whose rows these need padded: 13.3
+// Two projections of one row of 4608 bfloat16, 12288 columns: 39 us, 5.8 TB/s; 16 rows of 12288 bytes, 4608 columns: 14.7 us, 3.8 TB/s.
+// (Back to back, which leaves smaller weights in the last-level cache, 42.7 and 11.6 us, tiles of 64 rows whose contraction is cut into
+// runs 43.7 and 18.0; 1 x 1153, 1001 columns, whose rows these need padded: 13.3
 // against 5.9.)
 struct FewProduct {
     const char *a, *b0, *b1;
