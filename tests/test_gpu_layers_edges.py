@@ -89,10 +89,10 @@ def test_ties_of_products_with_the_weights():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("N,M,S", [(60, 72, 130), (1000, 72, 520), (1030, 72, 520), (1030, 75, 523)])
+@pytest.mark.parametrize("N,M,S", [(60, 72, 130), (1000, 72, 520), (1030, 72, 520), (1030, 75, 523), (600, 1300, 1000), (517, 545, 6559), (1300, 2000, 3000)])
 def test_infinite_gradients_of_centred_rows(N, M, S, dtype):
     """With mu, an infinite dg or du makes its row of dWg or dWu infinite with the sign that X - mu has, and NaN where X - mu is zero; in
-    bfloat16 on both sides of the 524288 entries from which on dg and du are one number."""
+    bfloat16 on both sides of the 524288 entries from which on dg and du are one number, in tiles cut into runs, whole ones, and both."""
     t, dt = TDT[dtype], FDT[dtype]
     rng = np.random.default_rng(N + M)
     low = wl.round_to_bf16 if dtype == "bf16" else (lambda x: x)
