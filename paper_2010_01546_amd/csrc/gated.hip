@@ -170,8 +170,8 @@ template <class T, bool FIX> struct WeightsEpilogue {        // rows below Sp ar
 };
 
 // The same in bfloat16 without FIX, with mu: D^T X - (D^T 1) mu^T is inf - inf where the formula has an infinity.  Once a wavefront has stored
-// its results it looks through the sums and the means behind them, and computes those again that come of one which is not finite; each lane
-// stores where it has stored before.  (2048 x 2304 x 6144 with D: 187 us, without this 185; looked for among the results, as FIX does, 201.)
+// its results it looks through the sums and the means behind them, and computes those again that come of one which is not finite, 16 x 16 at a time;
+// each lane stores where it has stored before.  (2048 x 2304 x 6144 with D: 187 us, without this 185; looked for among the results, as FIX does, 201.)
 struct CentredEpilogue : WeightsEpilogue<__bf16, false> {
     __device__ __forceinline__ void finish(int r0, int rows, int m0, int columns) const {
         const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
@@ -182,15 +182,35 @@ struct CentredEpilogue : WeightsEpilogue<__bf16, false> {
         for (int r = r0 + l16; r - l16 < r0 + rows; r += 16) {
             const int s = r >= Sp ? r - Sp : r;
             const float d = sums[min(r, 2 * Sp - 1)];
+            const bool none = has_nan(min(s, S - 1), r >= Sp, d);
             for (int m = m0 + 4 * q; m - 4 * q < m0 + columns; m += 16) {
                 float c[4];
                 tile_vector(mu, m, M, c);
+                if (__builtin_amdgcn_ballot_w64(!none && !(finite(d) && finite(c[0]) && finite(c[1]) && finite(c[2]) && finite(c[3]))) == 0) continue;
                 const floatx4 v = again_here(min(s, S - 1), r >= Sp, m);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (s < S && m + i < M && !(finite(d) && finite(c[i]))) (r >= Sp ? dWu : dWg)[(size_t)s * M + m + i] = (__bf16)v[i];
             }
         }
+    }
+    // whether the lane's column of D, one of 16 whose sums are d, has a NaN: its results are NaN then, and there already.  The four lanes of a
+    // column take its entries in turn, until there is nothing more to find.
+    __device__ __forceinline__ bool has_nan(int s, bool up, float d) const {
+        const int lane = threadIdx.x & 63;
+        const size_t at = (up ? (size_t)in.N * S : 0) + s;
+        bool mine = false, column = false;
+        for (int n = lane >> 4; n - (lane >> 4) < in.N && __builtin_amdgcn_ballot_w64(d != d && !column); n += 16) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const size_t e = (size_t)min(n + i, in.N - 1) * S;
+                const float p = (float)in.dH[e + s] * in.Z[e + at];
+                mine |= p != p;
+            }
+            const unsigned long long b = __builtin_amdgcn_ballot_w64(mine);
+            column = ((b | b >> 16 | b >> 32 | b >> 48) >> (lane & 15)) & 1;
+        }
+        return column;
     }
 };
 

@@ -146,6 +146,48 @@ def test_one_workspace_for_all_numbers_of_rows(dtype):
             assert torch.equal(a, c), N
 
 
+@pytest.mark.parametrize("N,M,S", [(1030, 75, 523), (600, 1300, 1000)])
+def test_nan_and_infinite_gradients_of_centred_rows(N, M, S):
+    """bfloat16, dg and du as one number: columns with a NaN, with infinities of one sign and of both, and a mean that is not finite."""
+    t, dt = torch.bfloat16, b.FW_BF16
+    rng = np.random.default_rng(N)
+    X, Wg, Wu, dH = (wl.round_to_bf16(rng.standard_normal(s).astype(np.float32)) for s in ((N, M), (S, M), (S, M), (N, S)))
+    mu = (X.mean(0) + 0.05).astype(np.float32)
+    Z = (0.3 + np.abs(rng.standard_normal((2, N, S)))).astype(np.float32)
+    dH[N - 1, 0], dH[0, 1], dH[5, 2:20] = np.nan, np.nan, np.inf
+    dH[7, 3], dH[N // 2, 40], dH[2, 41], dH[3, 41] = -np.inf, np.inf, np.inf, np.nan
+    Z[1, 4, 60] = np.nan                                          # in du alone
+    mu[11] = np.inf
+    dWg, dWu = (torch.empty(S, M, dtype=t, device=DEV) for _ in range(2))
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_GRAD, M, S, b.conv_desc(N, M), dt))
+    b.fw_gated_grad(dev(X, t), dt, N, M, S, dev(Wg, t), dev(Wu, t), dev(Z), dev(dH, t), dev(mu), None, dWg, dWu, None, None, ws)
+    torch.cuda.synchronize()
+    with np.errstate(all="ignore"):
+        want = lo.gated_grad_from(lo.f64(dH) * Z[0], lo.f64(dH) * Z[1], X, Wg, Wu, mu)
+    for got, w, what in zip((dWg, dWu), want[1:3], ("dWg", "dWu")):
+        got = got.float().cpu().numpy().astype(np.float64)
+        fine = np.isfinite(w)
+        assert np.array_equal(np.isnan(got), np.isnan(w)) and np.array_equal(got[np.isinf(w)], w[np.isinf(w)]), what
+        assert fine.any() and relF(got[fine], w[fine]) < 2 * HALF["bf16"], what
+
+
+def test_time_of_nan_gradients_of_centred_rows():
+    """A step full of NaN, as a diverged loss leaves it, takes about as long as any other: nothing is computed again for it."""
+    N, M, S, t, dt = 1000, 4608, 4000, torch.bfloat16, b.FW_BF16
+    X, W = torch.ones(N, M, device=DEV, dtype=t), torch.ones(S, M, device=DEV, dtype=t)
+    Z, dH, mu = torch.ones(2, N, S, device=DEV), torch.full((N, S), float("nan"), device=DEV, dtype=t), torch.ones(M, device=DEV)
+    dWg, dWu = torch.empty_like(W), torch.empty_like(W)
+    ws = workspace(b.fw_workspace_bytes(b.FW_OP_GATED_GRAD, M, S, b.conv_desc(N, M), dt))
+    begin, end = torch.cuda.Event(True), torch.cuda.Event(True)
+    for turn in range(2):
+        begin.record()
+        b.fw_gated_grad(X, dt, N, M, S, W, W, Z, dH, mu, None, dWg, dWu, None, None, ws)
+        end.record()
+        torch.cuda.synchronize()
+    assert bool(torch.isnan(dWg).all()) and bool(torch.isnan(dWu).all())
+    assert begin.elapsed_time(end) < 3                             # ms; 0.13 of finite ones, 6 where everything is computed again
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N,M,S", [(5, 64, 70), (200, 144, 300)])
 def test_scales_far_from_one(N, M, S, dtype):
